@@ -40,10 +40,14 @@
 #include <cstdint>
 
 #include "../../include/vbq.h"
+#include "vbq_quant.hpp"
 
 vbq_status vbq_detail_hip_status(hipError_t e);
 
 namespace {
+
+using vbq::exact_rne;
+using vbq::fp16_from_double;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -80,19 +84,6 @@ __device__ __forceinline__ u32x4 lds_u32x4(uint32_t addr) {
   return *(__attribute__((address_space(3))) u32x4*)(size_t)addr;
 }
 
-// fp16 value nearest to d >= 0 (round to nearest even), with one rounding:
-// d is first rounded to float by round-to-odd, which keeps enough bits (24 >=
-// 11 + 2) for the float -> fp16 conversion to round as if from d itself.
-__device__ __forceinline__ float fp16_from_double(double d) {
-  float f = (float)d;
-  if ((double)f != d) {
-    uint32_t b = __builtin_bit_cast(uint32_t, f);
-    if ((double)f > d) b -= 1u;  // the float below d (d > 0 here)
-    f = __builtin_bit_cast(float, b | 1u);
-  }
-  return (float)(_Float16)f;
-}
-
 // Components of a 4 x 32-bit vector are reinterpreted with __uint_as_float /
 // __float_as_uint: __builtin_bit_cast applied to a vector component (t.y)
 // reads the wrong component with this compiler.
@@ -102,17 +93,6 @@ struct Cand {   // one candidate width of one group
   float r;      // approximate 1/s (0 when s == 0)
   float qmax;
 };
-
-// Exact round-half-to-even of w/s given an estimate q0 within one of it.
-__device__ __forceinline__ float exact_rne(float w, float q0, float s) {
-  const float p = q0 * s;                          // exact: 9-bit times 11-bit significand
-  const float sg = w > p ? 1.0f : (w < p ? -1.0f : 0.0f);
-  const float b = __builtin_fmaf(0.5f, sg, q0) * s;  // midpoint toward w, exact
-  const bool beyond = sg > 0.0f ? (w > b) : (w < b);
-  const bool odd = (((int)q0) & 1) != 0;
-  const bool step = beyond || (w == b && odd);
-  return step ? q0 + sg : q0;
-}
 
 // The four candidates' scales of one group (section 3.1), from the group's
 // 64 weights in the lane's LDS row: max|w| in fp32 (exact), the 1-bit absmean
