@@ -486,6 +486,193 @@ vbq_status vbq_qat_logit_grad(int64_t n_groups, const float* W_dev,
                               float* dlogits_dev, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Between the products of a decode step: the residual sum and norm that make
+ * the next x, the cache of keys and values with the attention that reads it,
+ * and the choice of a token.  These calls follow the conventions at the top of
+ * this header; "type" is one of vbq_dtype.
+ * ------------------------------------------------------------------------- */
+typedef enum vbq_dtype { VBQ_F32 = 0, VBQ_F16 = 1, VBQ_BF16 = 2 } vbq_dtype;
+
+#define VBQ_NORM_MAX_K (((int64_t)1) << 24)
+
+/* Residual sum and root-mean-square norm: for each of n_rows rows of K elements
+ *   h = round(residual + y)   (the sum in fp32, rounded once to residual's type)
+ *   x = h / sqrt(mean(h^2) + eps) * weight   (fp32, rounded once to x's type).
+ *   y_dev       NULL: h = residual.   weight_dev (K elements)  NULL: ones.
+ *   h_dev       receives h in residual's type; NULL: not stored; may be
+ *               residual_dev itself (with ldh == ldr).  No other outputs and
+ *               inputs may overlap.
+ *   ldr, ldy, ldh, ldx   row strides in elements, >= K (ldy, ldh unused with
+ *               their pointers NULL).
+ * Pointers are aligned to their element; rows that begin at 16 bytes (pointer
+ * 16-byte aligned, strides and K multiples of 8) are read and written in
+ * 16-byte runs.  A row's sum is taken in a fixed order.  n_rows == 0 does
+ * nothing.  Errors: SHAPE (K outside [1, VBQ_NORM_MAX_K], n_rows outside
+ * [0, 2^31), a stride < K), UNSUPPORTED (unknown type, eps < 0), NONFINITE
+ * (eps), NULL (residual or x), BUFFER (misaligned), HIP. */
+vbq_status vbq_add_norm(int64_t n_rows, int64_t K, int32_t res_type,
+                        const void* residual_dev, int64_t ldr, int32_t y_type,
+                        const void* y_dev, int64_t ldy, int32_t weight_type,
+                        const void* weight_dev, float eps, void* h_dev,
+                        int64_t ldh, int32_t x_type, void* x_dev, int64_t ldx,
+                        void* stream);
+
+/* ---- a cache of keys and values held in 4 bits ----
+ * Each row (one position of one head, head_dim = D elements of the key and D of
+ * the value) is quantized in groups of 64 along D by the library's 4-bit rule
+ * (Eq. (1) at b = 4: s = fp16(max|w|/7), q = clip(round(w/s), -7, 7) against the
+ * stored s, round-half-to-even; codes u = q + 8; an all-zero group has s = 0).
+ * A group with NaN/Inf or with max|w| >= 7 * 65520 gets the scale NaN and gives
+ * NaN.  The cache is n_pages pages of VBQ_KV_PAGE positions
+ * of all heads; a page table per sequence says which pages hold its positions.
+ *
+ * Page layout, version 1.  Head h of page i begins at i * page_bytes + h * 68 * D:
+ *   keys' codes     32 D bytes: of each 16-position tile t = 0..3 (p / 16), code
+ *                   words (uint32) in the order [j / 4][lane][j % 4] (D = 64:
+ *                   [lane][j]), lane = 16 g + p % 16; word (j, g) holds elements
+ *                   32 j + 8 g .. + 7, pairs as in the packed weights (pair i in
+ *                   bits [4i, 4i+4) and [16+4i, 16+4i+4)).
+ *   values' codes   32 D bytes: of each 32-position block b = 0..1, words in the
+ *                   order [d / 64][lane][(d / 16) % 4], lane = 16 g + d % 16; a
+ *                   word holds element d of the block's slots 8 g .. 8 g + 7
+ *                   (in pairs as above), slot(p) = 8 ((p % 16) / 4) +
+ *                   4 ((p % 32) / 16) + p % 4.
+ *   keys' scales    fp16 [D / 64][2][32], by block and slot; then values' scales.
+ */
+#define VBQ_KV_MAGIC 0x3156514bu /* "KQV1" little-endian */
+#define VBQ_KV_VERSION 1u
+#define VBQ_KV_PAGE 64
+#define VBQ_KV_MAX_HEADS 1024
+#define VBQ_KV_MAX_GROUP 256          /* query heads of one kv head            */
+#define VBQ_KV_MAX_SEQS 65535
+#define VBQ_KV_MAX_ROWS (((int64_t)1) << 30)
+#define VBQ_KV_MAX_TABLE (1 << 24)    /* pages of one sequence                 */
+
+/* Host-side description of a cache (plain old data). */
+typedef struct vbq_kv_desc {
+  uint32_t magic, version;
+  int64_t n_pages;
+  int32_t n_heads, head_dim;          /* kv heads; 64, 128 or 256              */
+  uint64_t page_bytes, total_bytes;   /* the cache's device bytes              */
+} vbq_kv_desc;
+
+/* Fills *desc_out for a cache of n_pages pages.  Errors: NULL, SHAPE (n_pages
+ * outside [1, 2^31), n_heads outside [1, VBQ_KV_MAX_HEADS]), UNSUPPORTED (head_dim not 64,
+ * 128 or 256). */
+vbq_status vbq_kv_layout(int64_t n_pages, int32_t n_heads, int32_t head_dim,
+                         vbq_kv_desc* desc_out);
+
+/* The sequences of one call.  A call has n_rows rows (of k and v, or of q and
+ * out); sequence b owns rows row_start[b] .. row_start[b+1]-1, or max_rows rows
+ * each with row_start NULL (n_rows == n_seqs * max_rows then).  seq_len[b]
+ * counts its positions, this call's rows included: the last of its n rows is at
+ * position seq_len[b] - 1, its row r at seq_len[b] - n + r.  The arrays are device memory, read
+ * when the kernel runs.  Whatever they hold, rows outside [0, n_rows),
+ * positions below 0 or beyond table_stride pages, and pages outside
+ * [0, n_pages) are neither read nor written; what that leaves out is said at
+ * each call.  Rows of no sequence are left as they are. */
+typedef struct vbq_kv_batch {
+  int32_t n_seqs;                 /* 0 .. VBQ_KV_MAX_SEQS                      */
+  int32_t table_stride;           /* entries of a sequence in page_table       */
+  const int32_t* page_table;      /* device int32[n_seqs][table_stride]        */
+  const int32_t* row_start;       /* device int32[n_seqs + 1], or NULL         */
+  const int32_t* seq_len;         /* device int32[n_seqs]                      */
+  int64_t n_rows;                 /* 0 .. VBQ_KV_MAX_ROWS                      */
+  int32_t max_rows;               /* rows of the sequence with the most.  With */
+  int32_t max_len;                /* row_start it only sizes the launch, as    */
+} vbq_kv_batch;                   /* max_len (positions) does: a wrong value
+                                     costs time, not correctness               */
+
+/* Quantizes the rows of k and v into their positions' places in the cache.
+ * k, v: [n_rows][n_heads][D] of one type with row strides ldk, ldv and head
+ * strides hsk, hsv in elements (multiples of 8; pointers 16-byte aligned), such as the
+ * K and V columns of a fused projection's y.  No two sequences of a call may
+ * own the same page where they write, nor may calls that may overlap.  Rows at no position or page are
+ * dropped.  cache_dev: desc->total_bytes bytes, 256-byte aligned; its other
+ * positions keep their contents.  Errors: NULL, DESC, SHAPE, UNSUPPORTED
+ * (type), BUFFER, HIP. */
+vbq_status vbq_kv_append(const vbq_kv_desc* desc, void* cache_dev,
+                         const vbq_kv_batch* batch, int32_t type,
+                         const void* k_dev, int64_t ldk, int64_t hsk,
+                         const void* v_dev, int64_t ldv, int64_t hsv,
+                         void* stream);
+
+/* The cache's values at the positions of the call's rows: k_dev, v_dev float32
+ * [n_rows][n_heads][D], s * q (exact).  Rows at no position or page are left as
+ * they are.  For checking the cache, or for attention of one's own.  Errors:
+ * NULL, DESC, SHAPE, BUFFER (16-byte alignment), HIP. */
+vbq_status vbq_kv_dequant(const vbq_kv_desc* desc, const void* cache_dev,
+                          const vbq_kv_batch* batch, float* k_dev, float* v_dev,
+                          void* stream);
+
+/* Bytes of vbq_kv_attention's device workspace for this batch (0 where it
+ * needs none): a function of desc, n_q_heads and the batch's host fields.
+ * Errors: NULL, DESC, SHAPE. */
+vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
+                                           const vbq_kv_batch* batch,
+                                           int32_t n_q_heads, size_t* bytes);
+
+/* Attention of the call's query rows over the cache:
+ *   out[r][i] = sum_p softmax_p(scale * q[r][i] . k_p) v_p
+ * with k_p, v_p of kv head i / (n_q_heads / n_heads) as vbq_kv_dequant gives them,
+ * over the positions p from 0 up to the row's own (so its own key and value are to be
+ * appended first).  A row that sees no position (before position 0, or all its
+ * pages outside the cache) gives zeros; what the cache holds at
+ * positions that a row does not see does not matter, NaN included.
+ *   q_dev, out_dev   [n_rows][n_q_heads][D] of q_type, out_type, with row and
+ *             head strides in elements (multiples of 8; out's >= D), 16-byte
+ *             aligned; they may not overlap.  |q| below 2^100.
+ *   scale     2^-60 .. 2^60, e.g. 1/sqrt(D).
+ *   workspace_dev    16-byte aligned scratch of at least
+ *             vbq_kv_attention_workspace_size bytes, not shared by calls that
+ *             may overlap (NULL where that is 0).
+ * Sums and softmax statistics are fp32; a position's weight times its value
+ * scale is rounded to fp16 (2^-11 of the term), fp32 queries are taken as two
+ * fp16 terms, others as they are.  Sums are taken in a fixed order.
+ * Errors: NULL, DESC, SHAPE (n_q_heads not a multiple of n_heads, more
+ * than VBQ_KV_MAX_GROUP each, strides), UNSUPPORTED (types, scale), NONFINITE
+ * (scale), BUFFER, HIP. */
+vbq_status vbq_kv_attention(const vbq_kv_desc* desc, const void* cache_dev,
+                            const vbq_kv_batch* batch, int32_t n_q_heads,
+                            float scale, int32_t q_type, const void* q_dev,
+                            int64_t ldq, int64_t hsq, int32_t out_type,
+                            void* out_dev, int64_t ldo, int64_t hso,
+                            void* workspace_dev, size_t workspace_bytes,
+                            void* stream);
+
+#define VBQ_SAMPLE_MAX_V (((int64_t)1) << 20)
+#define VBQ_SAMPLE_MAX_ROWS (((int64_t)1) << 20)
+
+/* One token for each of M rows of V logits (row stride ld >= V elements).
+ * Candidates are the logits that are neither NaN nor -inf (where one is +inf,
+ * those equal to it weigh 1 and the others 0).  With z_max the largest,
+ * w_i = exp((z_i - z_max) / T) in double, held as whole multiples of 2^-43.
+ * In descending order of z, the lower index first among equals, a row keeps
+ *   its first top_k candidates (top_k <= 0 or >= V: all);
+ *   of these the shortest run from the start whose w sum to >= top_p times
+ *   their sum, one at least (top_p >= 1 or NaN: all);
+ *   of these the ones with w_i >= min_p (min_p > 1 counts as 1; <= 0 or NaN: all).
+ * The token is the first in index order at which the kept w's running sum exceeds
+ * u times their total (u clamped to [0, 1)); prob its share of that total.
+ * T not > 0 takes the first largest logit, with prob 1.  A row without
+ * candidates gives token -1 and prob 0.  Results are exact in these terms: they
+ * depend on no summation order.
+ *   temperature, top_p, min_p (float32[M]), top_k (int32[M]): device arrays,
+ *   NULL for T = 1 and no limit.   u float32[M].   token int32[M].
+ *   prob float32[M] or NULL.
+ *   workspace: vbq_sample_workspace_size bytes of device scratch, 16-byte aligned, not
+ *   shared by calls that may overlap.
+ * Errors: SHAPE (M outside [0, VBQ_SAMPLE_MAX_ROWS], V outside
+ * [1, VBQ_SAMPLE_MAX_V], ld), UNSUPPORTED (type), NULL, BUFFER, HIP. */
+vbq_status vbq_sample_workspace_size(int64_t M, int64_t V, size_t* bytes);
+vbq_status vbq_sample(int64_t M, int64_t V, int32_t type, const void* logits_dev,
+                      int64_t ld, const float* temperature_dev,
+                      const int32_t* top_k_dev, const float* top_p_dev,
+                      const float* min_p_dev, const float* u_dev,
+                      int32_t* token_dev, float* prob_dev, void* workspace_dev,
+                      size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement aid of the roofline harness (not part of the method).
  * ------------------------------------------------------------------------- */
 

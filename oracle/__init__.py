@@ -17,6 +17,8 @@ Modules
               fused kernels must reproduce (paper section 6).
   storage  -- packed-storage accounting, params * mean_bits / 8 (paper
               section 4, "Training", and Table 1).
+  decode   -- between the products of a decode step: residual sum and norm, the
+              4-bit cache and attention over it, the choice of a token.
   qat      -- differentiable bit selection: the Gumbel-Softmax mix of the four
               candidate reconstructions, the expected bit cost, the hardened
               widths and the logit-step gradient (paper sections 3.2-3.3 and
@@ -37,6 +39,6 @@ method fixes (hand-computed groups from Eq. (1), closed forms, invariants,
 brute force on tiny inputs); none is "parity unpinned".
 """
 
-from . import quant, layout, matmul, storage, qat  # noqa: F401
+from . import quant, layout, matmul, storage, qat, decode  # noqa: F401
 
-__all__ = ["quant", "layout", "matmul", "storage", "qat"]
+__all__ = ["quant", "layout", "matmul", "storage", "qat", "decode"]

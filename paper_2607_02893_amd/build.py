@@ -33,7 +33,7 @@ def _run(cmd, verbose):
 
 
 def build(verbose=False):
-    """Compile the packer (host C++), the decode, selection and measurement kernels (HIP, gfx950) into libvbq.so."""
+    """Compile the packer (host C++) and the kernels (HIP, gfx950) into libvbq.so."""
     hipcc = shutil.which("hipcc") or os.path.join(ROCM, "bin", "hipcc")
     clang = os.path.join(ROCM, "llvm", "bin", "clang++")
     if not os.path.exists(clang):
@@ -46,7 +46,7 @@ def build(verbose=False):
     _run([hipcc, f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", *DEVICE_FLAGS, "-c",
           os.path.join(CSRC, "vbq_kernels.hip"), "-o", kern_o], verbose)
     objs = [pack_o, kern_o]
-    for name in ("vbq_select", "vbq_measure"):
+    for name in ("vbq_select", "vbq_norm", "vbq_cache", "vbq_sample", "vbq_measure"):
         o = os.path.join(BUILD, name + ".o")
         _run([hipcc, f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", *DEVICE_FLAGS, "-c",
               os.path.join(CSRC, name + ".hip"), "-o", o], verbose)

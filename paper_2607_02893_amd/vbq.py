@@ -59,7 +59,9 @@ EXPORTS = ("vbq_status_string", "vbq_last_hip_error", "vbq_layout_version", "vbq
            "vbq_gemv_buckets", "vbq_gemm_small", "vbq_step_plan_bytes", "vbq_step_workspace_bytes",
            "vbq_step_plan", "vbq_step_run", "vbq_step_run_noalloc", "vbq_kernel_name", "vbq_gemv_buckets_kernel_name",
            "vbq_dequant",
-           "vbq_qat_workspace_size", "vbq_qat_forward", "vbq_qat_logit_grad", "vbq_read_ceiling")
+           "vbq_qat_workspace_size", "vbq_qat_forward", "vbq_qat_logit_grad", "vbq_add_norm", "vbq_kv_layout",
+           "vbq_kv_append", "vbq_kv_dequant", "vbq_kv_attention_workspace_size", "vbq_kv_attention",
+           "vbq_sample_workspace_size", "vbq_sample", "vbq_read_ceiling")
 # vbq_desc.flags (call options)
 Y_F16 = 1
 ONE_WAVE_PER_UNIT = 2
@@ -67,6 +69,9 @@ MAX_BUCKETS = 4
 QAT_MAX_GROUPS = 1 << 40
 QAT_WSOFT_BF16 = 1
 QAT_CANDIDATES = (1, 2, 4, 8)
+# vbq_dtype
+F32, F16, BF16 = 0, 1, 2
+KV_PAGE = 64
 
 
 class VbqDesc(ctypes.Structure):
@@ -95,6 +100,18 @@ class VbqBucket(ctypes.Structure):
 class VbqStepGemv(ctypes.Structure):
     _fields_ = [("desc", ctypes.POINTER(VbqDesc)), ("blob", ctypes.c_void_p), ("x", ctypes.c_void_p),
                 ("y", ctypes.c_void_p), ("rows", ctypes.c_void_p), ("y_len", ctypes.c_int64)]
+
+
+class VbqKvDesc(ctypes.Structure):
+    _fields_ = [("magic", ctypes.c_uint32), ("version", ctypes.c_uint32), ("n_pages", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_bytes", ctypes.c_uint64), ("total_bytes", ctypes.c_uint64)]
+
+
+class VbqKvBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("page_table", ctypes.c_void_p),
+                ("row_start", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("n_rows", ctypes.c_int64),
+                ("max_rows", ctypes.c_int32), ("max_len", ctypes.c_int32)]
 
 
 class VbqPackOpts(ctypes.Structure):
@@ -160,6 +177,26 @@ _lib.vbq_qat_forward.argtypes = [ctypes.c_int64, _P, _P, _P, ctypes.c_float, cty
                                  ctypes.c_size_t, _P]
 _lib.vbq_qat_logit_grad.restype = ctypes.c_int
 _lib.vbq_qat_logit_grad.argtypes = [ctypes.c_int64, _P, _P, _P, ctypes.c_float, ctypes.c_float, ctypes.c_int64, _P, _P]
+_I32, _I64, _F = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_lib.vbq_add_norm.restype = ctypes.c_int
+_lib.vbq_add_norm.argtypes = [_I64, _I64, _I32, _P, _I64, _I32, _P, _I64, _I32, _P, _F, _P, _I64, _I32, _P, _I64, _P]
+_lib.vbq_kv_layout.restype = ctypes.c_int
+_lib.vbq_kv_layout.argtypes = [_I64, _I32, _I32, ctypes.POINTER(VbqKvDesc)]
+_lib.vbq_kv_append.restype = ctypes.c_int
+_lib.vbq_kv_append.argtypes = [ctypes.POINTER(VbqKvDesc), _P, ctypes.POINTER(VbqKvBatch), _I32, _P, _I64, _I64, _P, _I64,
+                               _I64, _P]
+_lib.vbq_kv_dequant.restype = ctypes.c_int
+_lib.vbq_kv_dequant.argtypes = [ctypes.POINTER(VbqKvDesc), _P, ctypes.POINTER(VbqKvBatch), _P, _P, _P]
+_lib.vbq_kv_attention_workspace_size.restype = ctypes.c_int
+_lib.vbq_kv_attention_workspace_size.argtypes = [ctypes.POINTER(VbqKvDesc), ctypes.POINTER(VbqKvBatch), _I32,
+                                                 ctypes.POINTER(ctypes.c_size_t)]
+_lib.vbq_kv_attention.restype = ctypes.c_int
+_lib.vbq_kv_attention.argtypes = [ctypes.POINTER(VbqKvDesc), _P, ctypes.POINTER(VbqKvBatch), _I32, _F, _I32, _P, _I64, _I64,
+                                  _I32, _P, _I64, _I64, _P, ctypes.c_size_t, _P]
+_lib.vbq_sample_workspace_size.restype = ctypes.c_int
+_lib.vbq_sample_workspace_size.argtypes = [_I64, _I64, ctypes.POINTER(ctypes.c_size_t)]
+_lib.vbq_sample.restype = ctypes.c_int
+_lib.vbq_sample.argtypes = [_I64, _I64, _I32, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]
 
 
 class VbqError(RuntimeError):
@@ -652,6 +689,280 @@ def qat_logit_grad(W, grad, pi, tau, lam, n_bbar=None, dlogits=None, stream=None
                                    int(n if n_bbar is None else n_bbar), _dev_ptr(dlogits), _stream_handle(stream)),
            "vbq_qat_logit_grad")
     return dlogits
+
+
+# ------------------------------------------ between the products of a decode step
+
+if _torch is not None:
+    _DTYPES = {_torch.float32: F32, _torch.float16: F16, _torch.bfloat16: BF16}
+
+
+class _Launch:
+    """The device and stream of a call: tensors allocated inside belong to that
+    stream, so a freed scratch tensor is not handed out while the call runs.
+    `stream` None is the current stream of the tensors' device."""
+
+    def __init__(self, device, stream):
+        self._undo = None
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+            self._undo = _torch.cuda.stream(stream)
+        elif _torch.cuda.current_device() != device.index:
+            self._undo = _torch.cuda.device(device)
+        self._device = device
+
+    def __enter__(self):
+        if self._undo is not None:
+            self._undo.__enter__()
+        return _torch.cuda.current_stream(self._device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self._undo is not None:
+            self._undo.__exit__(*exc)
+
+
+def _dtype_of(t, name):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    return code
+
+
+def _gpu(t, name, device=None):
+    if t is None or not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    return t
+
+
+def _rows(t, name, shape, device=None):
+    """A GPU tensor of this shape whose last dimension is contiguous."""
+    _gpu(t, name, device)
+    if tuple(t.shape) != tuple(shape) or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        raise ValueError(f"{name} must be a {list(shape)} tensor with unit stride in the last dimension")
+    return t
+
+
+def _spread(t, name):
+    """A tensor that is written: no two of its elements share memory."""
+    reach = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n > 1):
+        if stride < reach:
+            raise ValueError(f"{name} must not overlap itself")
+        reach = stride * (size - 1) + reach
+    return t
+
+
+def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=None, stream=None):
+    """Residual sum and root-mean-square norm (vbq_add_norm): h = round(residual + y) in
+    residual's type, x = h / sqrt(mean(h^2) + eps) * weight.
+
+    residual, y: [..., K] seen as [rows, K] (2-d tensors may have padded rows); y None: h = residual.
+    weight: contiguous [K] or None.  h: a tensor to write the sum into (residual
+    itself for in place); None allocates it, False leaves it out.  x is x_dtype (float16, the products' input).
+    Returns (x, h), h None where left out (and residual itself where y is None and no h is given)."""
+    _gpu(residual, "residual")
+    dev, K = residual.device, residual.shape[-1]
+    shape = residual.shape
+    two = len(shape) == 2
+    if x_dtype is None:
+        x_dtype = _torch.float16 if x is None else x.dtype
+    if not two:
+        for t, name in ((residual, "residual"), (y, "y"), (x, "x"), (h if h is not False else None, "h")):
+            if t is not None and not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous unless it has two dimensions")
+    for t, name in ((residual, "residual"), (y, "y")):
+        if t is not None:
+            _rows(t, name, shape, dev)
+    if weight is not None:
+        _rows(weight, "weight", (K,), dev)
+    with _Launch(dev, stream) as s:
+        if x is None:
+            x = _torch.empty(shape, dtype=x_dtype, device=dev)
+        if h is None:
+            h = residual if y is None else _torch.empty(shape, dtype=residual.dtype, device=dev)
+        _spread(_rows(x, "x", shape, dev), "x")
+        if h is not False and h is not residual:
+            _spread(_rows(h, "h", shape, dev), "h")
+            if h.dtype != residual.dtype:
+                raise ValueError("h must have residual's type")
+        if x.dtype != x_dtype:
+            raise ValueError(f"x must be {x_dtype}")
+        n = residual.numel() // K if K else 0
+        row = lambda t: (t.stride(0) if two and n > 1 else K)  # noqa: E731
+        keep = None if h is False or (h is residual and y is None) else h
+        if keep is residual:
+            _spread(residual, "residual")
+        _check(_lib.vbq_add_norm(n, K, _dtype_of(residual, "residual"), residual.data_ptr(), row(residual),
+                                 0 if y is None else _dtype_of(y, "y"), None if y is None else y.data_ptr(),
+                                 0 if y is None else row(y), 0 if weight is None else _dtype_of(weight, "weight"),
+                                 None if weight is None else weight.data_ptr(), eps,
+                                 None if keep is None else keep.data_ptr(), 0 if keep is None else row(keep),
+                                 _dtype_of(x, "x"), x.data_ptr(), row(x), s), "vbq_add_norm")
+    return x, (None if h is False else h)
+
+
+class KVBatch:
+    """The sequences of one call on a cache (vbq_kv_batch).
+
+    page_table: int32 [n_seqs, pages] device tensor; seq_len: int32 [n_seqs],
+    positions of each sequence with the call's rows.  rows: int32
+    [n_seqs + 1], the first row of each sequence and the end of the last; None:
+    max_rows rows each.  n_rows: rows of the call's tensors (n_seqs * max_rows
+    by default).  max_rows, max_len: the most rows and positions of a sequence
+    (with `rows`, and for max_len always, they size the launch only; max_len
+    defaults to what the table holds).  The tensors may change between calls
+    (a captured graph reads them anew); they must stay alive until the call has run."""
+
+    def __init__(self, page_table, seq_len, rows=None, n_rows=None, max_rows=1, max_len=None):
+        dev = _gpu(page_table, "page_table").device
+        if page_table.dim() != 2 or seq_len is None or seq_len.dim() != 1 or page_table.shape[0] != seq_len.shape[0]:
+            raise ValueError("page_table must be [n_seqs, pages] and seq_len [n_seqs]")
+        n, pages = page_table.shape
+        _need(page_table, "page_table", _torch.int32)
+        _need(seq_len, "seq_len", _torch.int32, n, dev)
+        if rows is not None:
+            _need(rows, "rows", _torch.int32, n + 1, dev)
+            if n_rows is None:
+                raise ValueError("rows needs n_rows")
+        self.device, self.n_seqs, self.max_rows = dev, n, int(max_rows)
+        self.n_rows = n * self.max_rows if n_rows is None else int(n_rows)
+        self.page_table, self.seq_len, self.rows = page_table, seq_len, rows
+        self.max_len = min(pages * KV_PAGE, 2 ** 31 - 1) if max_len is None else int(max_len)
+        for name in ("n_rows", "max_rows", "max_len"):
+            if not 0 <= getattr(self, name) < 2 ** 31:
+                raise ValueError(f"{name} must be in [0, 2^31)")
+        self.c = VbqKvBatch(n, pages, page_table.data_ptr(), None if rows is None else rows.data_ptr(),
+                            seq_len.data_ptr(), self.n_rows, self.max_rows, self.max_len)
+        self._ref = ctypes.byref(self.c)
+
+
+class KVCache:
+    """A cache of keys and values in 4 bits, in device memory (vbq_kv_layout): n_pages
+    pages of KV_PAGE positions, n_heads kv heads of head_dim elements."""
+
+    def __init__(self, n_pages, n_heads, head_dim, device="cuda"):
+        self.desc = VbqKvDesc()
+        _check(_lib.vbq_kv_layout(n_pages, n_heads, head_dim, ctypes.byref(self.desc)), "vbq_kv_layout")
+        self.n_pages, self.n_heads, self.head_dim = n_pages, n_heads, head_dim
+        self.data = _torch.zeros(self.desc.total_bytes, dtype=_torch.uint8, device=device)
+        if self.data.data_ptr() % 256:
+            raise VbqError(7, "KVCache")
+        self._ref = ctypes.byref(self.desc)
+
+    @property
+    def nbytes(self):
+        return int(self.desc.total_bytes)
+
+    def _of_rows(self, t, name, batch, heads, dtype=None):
+        _rows(t, name, (batch.n_rows, heads, self.head_dim), self.data.device)
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}")
+        return t
+
+    def _batch(self, batch):
+        if batch.device != self.data.device:
+            raise ValueError(f"the batch is on {batch.device}, the cache on {self.data.device}")
+        return batch._ref
+
+    def append(self, k, v, batch, stream=None):
+        """Quantizes rows k, v [n_rows, n_heads, head_dim] (one type; views such as the columns of a fused
+        projection's y will do: strides multiples of 8, 16-byte aligned) into the cache (vbq_kv_append)."""
+        self._of_rows(k, "k", batch, self.n_heads)
+        self._of_rows(v, "v", batch, self.n_heads, k.dtype)
+        ref = self._batch(batch)
+        with _Launch(self.data.device, stream) as s:
+            _check(_lib.vbq_kv_append(self._ref, self.data.data_ptr(), ref, _dtype_of(k, "k"), k.data_ptr(), k.stride(0),
+                                      k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), s), "vbq_kv_append")
+
+    def dequant(self, batch, k=None, v=None, stream=None):
+        """(k, v), float32 [n_rows, n_heads, head_dim]: the values the cache holds at the
+        positions of the call's rows (vbq_kv_dequant); rows without a place are left as they are (zeros where allocated here)."""
+        dev, shape, ref = self.data.device, (batch.n_rows, self.n_heads, self.head_dim), self._batch(batch)
+        with _Launch(dev, stream) as s:
+            k = _torch.zeros(shape, dtype=_torch.float32, device=dev) if k is None else k
+            v = _torch.zeros(shape, dtype=_torch.float32, device=dev) if v is None else v
+            for t, name in ((k, "k"), (v, "v")):
+                _need(self._of_rows(t, name, batch, self.n_heads), name, _torch.float32)
+            _check(_lib.vbq_kv_dequant(self._ref, self.data.data_ptr(), ref, k.data_ptr(), v.data_ptr(), s), "vbq_kv_dequant")
+        return k, v
+
+    def attention_workspace_size(self, batch, n_q_heads):
+        nbytes = ctypes.c_size_t(0)
+        _check(_lib.vbq_kv_attention_workspace_size(self._ref, batch._ref, n_q_heads, ctypes.byref(nbytes)),
+               "vbq_kv_attention_workspace_size")
+        return nbytes.value
+
+    def attention(self, q, batch, scale=None, out=None, out_dtype=None, workspace=None, stream=None):
+        """Attention of q [n_rows, n_q_heads, head_dim] over the cache (vbq_kv_attention): each row
+        sees its sequence's positions up to its own.  scale: 1/sqrt(head_dim) by default.  out: q's type, or
+        out_dtype; rows of no sequence are left as they are (uninitialised where out is allocated here).
+        workspace: uint8 tensor of attention_workspace_size bytes, allocated where not given."""
+        dev, ref = self.data.device, self._batch(batch)
+        heads = q.shape[1] if getattr(q, "dim", lambda: 0)() == 3 else 0
+        self._of_rows(q, "q", batch, heads)
+        if out_dtype is None:
+            out_dtype = q.dtype if out is None else out.dtype
+        with _Launch(dev, stream) as s:
+            if out is None:
+                out = _torch.empty(q.shape, dtype=out_dtype, device=dev)
+            _spread(self._of_rows(out, "out", batch, heads, out_dtype), "out")
+            need = self.attention_workspace_size(batch, heads)
+            if workspace is None and need:
+                workspace = _torch.empty(need, dtype=_torch.uint8, device=dev)
+            elif workspace is not None:
+                _need(workspace, "workspace", _torch.uint8, None, dev)
+            _check(_lib.vbq_kv_attention(self._ref, self.data.data_ptr(), ref, heads,
+                                         self.head_dim ** -0.5 if scale is None else scale, _dtype_of(q, "q"), q.data_ptr(),
+                                         q.stride(0), q.stride(1), _dtype_of(out, "out"), out.data_ptr(), out.stride(0),
+                                         out.stride(1), None if workspace is None else workspace.data_ptr(),
+                                         0 if workspace is None else workspace.numel(), s), "vbq_kv_attention")
+        return out
+
+
+def sample_workspace_size(M, V):
+    nbytes = ctypes.c_size_t(0)
+    _check(_lib.vbq_sample_workspace_size(M, V, ctypes.byref(nbytes)), "vbq_sample_workspace_size")
+    return nbytes.value
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=None, workspace=None,
+           stream=None):
+    """One token a row (vbq_sample): logits [M, V] (rows may be padded), u float32 [M] the
+    random numbers in [0, 1), temperature / top_p / min_p float32 [M] and top_k int32 [M] device tensors or None.
+    probs: a tensor to write into, None to allocate, False to leave out.  Returns (tokens int32 [M], probs float32 [M] or None)."""
+    _gpu(logits, "logits")
+    dev = logits.device
+    if logits.dim() != 2:
+        raise ValueError("logits must be [M, V]")
+    M, V = logits.shape
+    _rows(logits, "logits", (M, V), dev)
+    _need(u, "u", _torch.float32, M, dev)
+    for t, name, dtype in ((temperature, "temperature", _torch.float32), (top_k, "top_k", _torch.int32),
+                           (top_p, "top_p", _torch.float32), (min_p, "min_p", _torch.float32)):
+        if t is not None:
+            _need(t, name, dtype, M, dev)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    with _Launch(dev, stream) as s:
+        if tokens is None:
+            tokens = _torch.empty(M, dtype=_torch.int32, device=dev)
+        if probs is None:
+            probs = _torch.empty(M, dtype=_torch.float32, device=dev)
+        probs = None if probs is False else probs
+        _need(tokens, "tokens", _torch.int32, M, dev)
+        if probs is not None:
+            _need(probs, "probs", _torch.float32, M, dev)
+        need = sample_workspace_size(M, V)
+        if workspace is None and need:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=dev)
+        elif workspace is not None:
+            _need(workspace, "workspace", _torch.uint8, None, dev)
+        _check(_lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V,
+                               ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p), u.data_ptr(), tokens.data_ptr(),
+                               ptr(probs), ptr(workspace), 0 if workspace is None else workspace.numel(), s), "vbq_sample")
+    return tokens, probs
 
 
 def raw_qat_logit_grad(n_groups, W_ptr, grad_ptr, pi_ptr, tau, lam, n_bbar, d_ptr, stream_ptr):
