@@ -630,7 +630,7 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
  * scale is rounded to fp16 (2^-11 of the term), fp32 queries are taken as two
  * fp16 terms, others as they are.  Sums are taken in a fixed order.
  * Errors: NULL, DESC, SHAPE (n_q_heads not a multiple of n_heads, more
- * than VBQ_KV_MAX_GROUP each, strides), UNSUPPORTED (types, scale), NONFINITE
+ * than VBQ_KV_MAX_GROUP each, n_rows times their number a kv head above 2^30, strides), UNSUPPORTED (types, scale), NONFINITE
  * (scale), BUFFER, HIP. */
 vbq_status vbq_kv_attention(const vbq_kv_desc* desc, const void* cache_dev,
                             const vbq_kv_batch* batch, int32_t n_q_heads,

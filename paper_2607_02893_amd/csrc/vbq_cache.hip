@@ -56,6 +56,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;           // waves of a workgroup
+constexpr int kMaxSplits = 64;      // parts of a sequence's positions: a lane each in the join
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // ------------------------------------------------------------------ element types
@@ -269,7 +270,8 @@ struct AttnArgs {
   void* out;
   int64_t ldq, hsq, ldo, hso;
   float scale;
-  int32_t tiles, splits;  // row tiles of the grid, parts of the positions
+  int32_t splits;         // parts of the positions
+  int32_t split_pages;    // pages of a part
   float* part;            // [row * query heads + head][split][D], then as many pairs (bias, sum)
 };
 
@@ -375,14 +377,23 @@ struct Rows {
   // The row's elements times a power of two that puts the largest into [2^14, 2^15);
   // fp32 rows are split into two fp16 terms, the others are exact in one (unless
   // smaller than 2^-34 of the row's largest).
-  __device__ __forceinline__ void load(const AttnArgs& a, int nt, int64_t row, int head, bool on, int g) {
+  __device__ __forceinline__ void load(const AttnArgs& a, int nt, int64_t row, uint32_t head, int g) {
     float f[D / 32][8];
     float amax = 0.0f;
+    const int64_t at = row * a.ldq + (int64_t)head * a.hsq + 8 * g;
+    // (rows that are none take the call's first: any will do, they are not stored)
+    if constexpr (kTwoTerms) {
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) load8(a.q, at + 32 * j, VBQ_F32, f[j]);
+    } else if (a.q_type == VBQ_F16) {
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) load8(a.q, at + 32 * j, VBQ_F16, f[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) load8(a.q, at + 32 * j, VBQ_BF16, f[j]);
+    }
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[j][i] = 0.0f;
-      if (on) load8(a.q, row * a.ldq + (int64_t)head * a.hsq + 32 * j + 8 * g, a.q_type, f[j]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) amax = __builtin_fmaxf(amax, __builtin_fabsf(f[j][i]));
     }
@@ -423,11 +434,11 @@ struct Rows {
     return (mu[nt] == -__builtin_inff() ? 0.0f : mu[nt]) + (float)(e - 21);
   }
 
-  // One block of 32 positions from `pos` on; kEdge: some of them are hidden from some row.
-  // Hidden positions get the score -inf and the value scale 0, whatever their memory holds.
-  template <bool kEdge>
-  __device__ __forceinline__ void block(Block<D>& k, int pos, int end, int g) {
-    if constexpr (kEdge) {
+  // One block of 32 positions from `pos` on; edge: some of them are hidden from some row.
+  // Hidden positions get the score -inf and their product with the value scale is 0,
+  // whatever their memory holds.
+  __device__ __forceinline__ void block(Block<D>& k, int pos, int end, int g, bool edge) {
+    if (edge) {
 #pragma unroll
       for (int grp = 0; grp < kGroups; ++grp) {
 #pragma unroll
@@ -462,8 +473,17 @@ struct Rows {
           float s = 0.0f;
 #pragma unroll
           for (int grp = 0; grp < kGroups; ++grp) s = __builtin_fmaf((float)__builtin_bit_cast(f16x8, k.ks[grp])[4 * t + i], acc[nt][grp][i], s);
-          if (kEdge && pos + 16 * t + 4 * g + i >= visible[nt]) s = -__builtin_inff();
           x[nt][4 * t + i] = s;
+        }
+      }
+    }
+
+    if (edge) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (pos + 16 * (i >> 2) + 4 * g + (i & 3) >= visible[nt]) x[nt][i] = -__builtin_inff();
         }
       }
     }
@@ -512,11 +532,20 @@ struct Rows {
       for (int i = 0; i < 8; ++i) {
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nt][i], c[nt], -b));
         sum[nt] += p;
-        const bool hidden = kEdge && pos + 16 * (i >> 2) + 4 * g + (i & 3) >= visible[nt];
 #pragma unroll
-        for (int grp = 0; grp < kGroups; ++grp) {
-          const _Float16 vs = hidden ? (_Float16)0.0f : __builtin_bit_cast(f16x8, k.vs[grp])[i];
-          w[nt][grp][i] = (_Float16)__builtin_fmaf(p, (float)vs, 0.0f);
+        for (int grp = 0; grp < kGroups; ++grp)
+          w[nt][grp][i] = (_Float16)__builtin_fmaf(p, (float)__builtin_bit_cast(f16x8, k.vs[grp])[i], 0.0f);
+      }
+    }
+    if (edge) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (pos + 16 * (i >> 2) + 4 * g + (i & 3) >= visible[nt]) {
+#pragma unroll
+            for (int grp = 0; grp < kGroups; ++grp) w[nt][grp][i] = (_Float16)0.0f;
+          }
         }
       }
     }
@@ -539,60 +568,60 @@ __device__ __forceinline__ void store_bias(const AttnArgs& a, int64_t row_head, 
   at[1] = sum;
 }
 
+// Row tiles of a wave that has rows of its own: what its registers hold.
+constexpr int wave_tiles(int D) { return D == 256 ? 1 : 2; }
+constexpr int waves_per_simd(int D, int NT) { return D * NT <= 64 ? 4 : D * NT <= 128 ? 3 : 2; }
+
 // kWaveRows: the four waves take different rows and walk the same positions;
 // otherwise they take the same rows and every fourth page each, and join at the end.
 template <int D, int NT, bool kTwoTerms, bool kWaveRows>
-__global__ __launch_bounds__(kWaves * 64) void vbq_kv_attention_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_attention_kernel(AttnArgs a) {
   using P = PageOf<D>;
   constexpr int kRows = 16 * NT * (kWaveRows ? kWaves : 1);
   __shared__ __attribute__((aligned(16))) float o_lds[kWaveRows ? 1 : kWaves][kWaveRows ? 1 : kRows][kWaveRows ? 4 : D + 4];
   __shared__ float bias_lds[kWaveRows ? 1 : kWaves][kWaveRows ? 1 : kRows], sum_lds[kWaveRows ? 1 : kWaves][kWaveRows ? 1 : kRows];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, g = lane >> 4;
-  int64_t at = blockIdx.x;
-  const int h = (int)(at % a.heads);
-  at /= a.heads;
-  const int split = (int)(at % a.splits);
-  at /= a.splits;
-  const int b = (int)(at % a.batch.n_seqs);
+  const uint32_t h = blockIdx.x % (uint32_t)a.heads, split = blockIdx.x / (uint32_t)a.heads, group = (uint32_t)a.group;
+  const int b = (int)blockIdx.y;
   const Seq s = seq_of(a.batch, b);
-  const int64_t n_rows = s.n * a.group;
-  const int hq0 = h * a.group;
+  const uint32_t n_rows = (uint32_t)s.n * group;  // (below 2^31)
+  const uint32_t hq0 = h * group;
 
   // the last tiles see the most positions: they start first
-  for (int64_t tile = a.tiles - 1 - at / a.batch.n_seqs; tile * kRows < n_rows; tile += a.tiles) {
-    const int64_t base = tile * kRows + (kWaveRows ? wave * 16 * NT : 0);
+  for (uint32_t tile = gridDim.z - 1 - blockIdx.z; tile * kRows < n_rows; tile += gridDim.z) {
+    const uint32_t base = tile * kRows + (kWaveRows ? wave * 16 * NT : 0);
     Rows<D, NT, kTwoTerms> r;
     r.e = 0;
-    const int64_t last = base + 16 * NT < n_rows ? base + 16 * NT : n_rows;
-    auto seen = [&](int64_t i) {
-      const int64_t v = s.pos0 + i / a.group + 1;
+    const uint32_t last = base + 16 * NT < n_rows ? base + 16 * NT : n_rows;
+    auto seen = [&](uint32_t row) {
+      const int64_t v = s.pos0 + row + 1;
       return (int)(v < 0 ? 0 : v < s.end ? v : s.end);
     };
-    const int least = base < n_rows ? seen(base) : 0, most = base < n_rows ? seen(last - 1) : 0;
+    const int least = base < n_rows ? seen(base / group) : 0, most = base < n_rows ? seen((last - 1) / group) : 0;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int64_t i = base + 16 * nt + (lane & 15);
+      const uint32_t i = base + 16 * nt + (lane & 15), row = i / group;
       const bool on = i < n_rows;
-      r.visible[nt] = on ? seen(i) : 0;
-      r.load(a, nt, s.row0 + (on ? i / a.group : 0), hq0 + (on ? (int)(i % a.group) : 0), on, g);
+      r.visible[nt] = on ? seen(row) : 0;
+      r.load(a, nt, s.row0 + (on ? row : 0), hq0 + (on ? i - row * group : 0), g);
     }
-    const int pages = (most + kPage - 1) / kPage, per = (pages + a.splits - 1) / a.splits;
-    const int stop = (split + 1) * per < pages ? (split + 1) * per : pages, step = kWaveRows ? 1 : kWaves;
-    int page = split * per + (kWaveRows ? 0 : wave);
+    const int pages = (most + kPage - 1) / kPage, least_per = (pages + a.splits - 1) / a.splits;
+    const int per = a.split_pages > least_per ? a.split_pages : least_per;
+    const int stop = (int)(split + 1) * per < pages ? (int)(split + 1) * per : pages, step = kWaveRows ? 1 : kWaves;
+    int page = (int)split * per + (kWaveRows ? 0 : wave);
     int64_t next = page < stop ? page_id(a.batch, a.n_pages, b, page) : -1;
     for (; page < stop; page += step) {
       const int64_t id = next;
       if (page + step < stop) next = page_id(a.batch, a.n_pages, b, page + step);
       if (id < 0) continue;
       const uint8_t* from = a.cache + (id * a.heads + h) * (int64_t)P::kBytes;
-#pragma unroll
+#pragma unroll 1
       for (int half = 0; half < 2; ++half) {
         const int pos = page * kPage + 32 * half;
         if (pos >= most) break;
         Block<D> k;
         load_block<D>(k, from, half, lane);
-        if (pos + 32 <= least) r.template block<false>(k, pos, (int)s.end, g);
-        else r.template block<true>(k, pos, (int)s.end, g);
+        r.block(k, pos, (int)s.end, g, pos + 32 > least);
       }
     }
 
@@ -600,17 +629,20 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_attention_kernel(AttnArgs 
     if constexpr (kWaveRows) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int64_t i = base + 16 * nt + (lane & 15);
+        const uint32_t i = base + 16 * nt + (lane & 15);
         const float sum = group_sum(r.sum[nt]);
         if (i >= n_rows) continue;
-        const int64_t row = s.row0 + i / a.group;
-        const int hq = hq0 + (int)(i % a.group);
+        const int64_t row = s.row0 + i / group;
+        const int64_t hq = hq0 + i % group;
         if (a.splits == 1) {
-          const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+          const float f = sum == 0.0f ? 0.0f : 1.0f / sum;  // (the sums of a row that sees nothing are 0)
+          const int64_t at = row * a.ldo + hq * a.hso + 4 * g;
+          if (a.out_type == VBQ_F32) {
 #pragma unroll
-          for (int d = 0; d < D / 16; ++d) {
-            const f32x4 v = sum == 0.0f ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : r.o[nt][d] * f;
-            store4(a.out, row * a.ldo + hq * a.hso + 16 * d + 4 * g, a.out_type, v);
+            for (int d = 0; d < D / 16; ++d) *(f32x4*)((float*)a.out + at + 16 * d) = r.o[nt][d] * f;
+          } else {
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) store4(a.out, at + 16 * d, a.out_type, r.o[nt][d] * f);
           }
         } else {
           const int64_t rh = row * heads + hq;
@@ -634,7 +666,7 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_attention_kernel(AttnArgs 
       __syncthreads();
       constexpr int kLanes = 256 / kRows, kEach = D / kLanes;  // lanes of a row, elements of a lane
       const int i = (int)threadIdx.x / kLanes, sub = (int)threadIdx.x % kLanes;
-      const int64_t ri = base + i;
+      const uint32_t ri = base + i;
       if (ri < n_rows) {
         float top = -__builtin_inff(), f[kWaves], sum = 0.0f;
 #pragma unroll
@@ -648,8 +680,8 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_attention_kernel(AttnArgs 
           f[w] = f[w] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(f[w] - top);
           sum += sum_lds[w][i] * f[w];
         }
-        const int64_t row = s.row0 + ri / a.group;
-        const int hq = hq0 + (int)(ri % a.group);
+        const int64_t row = s.row0 + ri / group;
+        const int64_t hq = hq0 + ri % group;
         const int64_t rh = row * heads + hq;
         const float scale = a.splits > 1 ? 1.0f : 1.0f / sum;
         if (a.splits > 1 && sub == 0) store_bias<D>(a, rh, split, top == -__builtin_inff() ? 0.0f : top, sum);
@@ -670,46 +702,54 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_attention_kernel(AttnArgs 
   }
 }
 
-// A row's parts joined: one workgroup a row and head, each wave every fourth part.
+// A row's parts joined: one workgroup a row and head, a wave's lanes over the parts' biases, then
+// 16 bytes a lane of several parts side by side, all loads before the first use.
 template <int D>
 __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
-  constexpr int kLanes = D / 4;             // lanes of a part, four elements each
-  constexpr int kSide = 256 / kLanes;       // parts side by side
+  constexpr int kLanes = D / 4;                   // lanes of a part, four elements each
+  constexpr int kSide = 256 / kLanes;             // parts side by side
+  constexpr int kTurns = kMaxSplits / kSide;
   __shared__ __attribute__((aligned(16))) float o_lds[kSide][D];
-  __shared__ float sum_lds[kSide];
+  __shared__ float f_lds[kMaxSplits];
   const int heads = a.heads * a.group;
-  int64_t at = blockIdx.x;
-  const int hq = (int)(at % heads);
-  at /= heads;
-  const int b = (int)(at % a.batch.n_seqs);
+  const int hq = (int)blockIdx.x, b = (int)blockIdx.y;
   const Seq s = seq_of(a.batch, b);
-  const int side = (int)threadIdx.x / kLanes, el = 4 * ((int)threadIdx.x % kLanes);
-  const int64_t rows = a.batch.n_rows;
-  for (int64_t i = at / a.batch.n_seqs; i < s.n; i += a.batch.max_rows) {
+  const int tid = (int)threadIdx.x, side = tid / kLanes, el = 4 * (tid % kLanes);
+  for (int64_t i = blockIdx.z; i < s.n; i += gridDim.z) {
     const int64_t rh = (s.row0 + i) * heads + hq;
-    const float* bias = a.part + rows * heads * a.splits * (int64_t)D + 2 * rh * a.splits;
-    float top = -__builtin_inff();
-    for (int p = 0; p < a.splits; ++p) top = bias[2 * p + 1] == 0.0f ? top : __builtin_fmaxf(top, bias[2 * p]);
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 part[kTurns];
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+      const int p = side + j * kSide;
+      part[j] = *(const f32x4*)(a.part + (rh * a.splits + (p < a.splits ? p : 0)) * D + el);
+    }
     float sum = 0.0f;
-#pragma unroll 4
-    for (int p = side; p < a.splits; p += kSide) {
-      const f32x4 part = *(const f32x4*)(a.part + (rh * a.splits + p) * D + el);
-      const float n = bias[2 * p + 1], f = n == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(bias[2 * p] - top);
-      sum += n * f;
-      v += part * f;
+    if (tid < kMaxSplits) {  // (the first wave)
+      const float* pair = a.part + a.batch.n_rows * heads * a.splits * (int64_t)D + 2 * rh * a.splits;
+      const bool on = tid < a.splits;
+      const float n = on ? pair[2 * tid + 1] : 0.0f, bias = on && n != 0.0f ? pair[2 * tid] : -__builtin_inff();
+      float top = bias;
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, d, 64));
+      const float f = n == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(bias - top);
+      f_lds[tid] = f;
+      sum = n * f;
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    }
+    __syncthreads();
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+      const float f = f_lds[side + j * kSide];
+      if (f != 0.0f) v += part[j] * f;  // (0 also where there is no part)
     }
     *(f32x4*)&o_lds[side][el] = v;
-    if (el == 0) sum_lds[side] = sum;
     __syncthreads();
-    if ((int)threadIdx.x < kLanes) {
-      sum = 0.0f;
+    if (tid < kLanes) {
       v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < kSide; ++j) {
-        sum += sum_lds[j];
-        v += *(const f32x4*)&o_lds[j][el];
-      }
+      for (int j = 0; j < kSide; ++j) v += *(const f32x4*)&o_lds[j][el];
       store4(a.out, (s.row0 + i) * a.ldo + hq * a.hso + el, a.out_type, sum == 0.0f ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : v * (1.0f / sum));
     }
     __syncthreads();
@@ -718,8 +758,8 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
 
 // ------------------------------------------------------------------ host side
 
-constexpr int kMaxSplits = 64;
 constexpr int64_t kMaxGrid = (int64_t)1 << 30;
+constexpr int64_t kSplitGrid = 2048;
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
 bool known(int32_t type) { return type == VBQ_F32 || type == VBQ_F16 || type == VBQ_BF16; }
@@ -754,26 +794,33 @@ Batch batch_of(const vbq_kv_batch* b) {
 
 struct Plan {
   bool wave_rows;
-  int tiles, splits;
+  int tiles, splits, split_pages;
 };
 
 Plan plan_of(const vbq_kv_desc* d, const vbq_kv_batch* b, int group) {
   Plan p;
   const int64_t rows = (b->max_rows < b->n_rows ? b->max_rows : b->n_rows) * (int64_t)group;
   p.wave_rows = rows > 64;
-  const int64_t per = p.wave_rows ? 128 : 16, tiles = (rows + per - 1) / per;
-  const int64_t units = (int64_t)b->n_seqs * d->n_heads, most = kMaxGrid / kMaxSplits / units;
-  p.tiles = (int)(tiles < most ? tiles : most > 1 ? most : 1);
-  const int64_t base = units * p.tiles, pages = ((int64_t)b->max_len + kPage - 1) / kPage;
-  int64_t s = base >= 512 ? 1 : (1024 + base - 1) / base;
-  if (s > (pages + 3) / 4) s = (pages + 3) / 4;
-  p.splits = (int)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
+  const int64_t per = p.wave_rows ? 16 * kWaves * wave_tiles(d->head_dim) : 16, tiles = (rows + per - 1) / per;
+  const int64_t units = (int64_t)b->n_seqs * d->n_heads, most = kMaxGrid / kMaxSplits / units;  // (the kernel's loop takes the rest)
+  p.tiles = (int)(tiles < 16384 ? tiles : 16384);
+  if (p.tiles > most) p.tiles = most > 1 ? (int)most : 1;
+  // Parts of equal size whatever a sequence's length, so that long sequences of a ragged batch get
+  // more workgroups: up to kSplitGrid if all were max_len long, no part below a page a wave.
+  const int64_t base = units * p.tiles, pages = ((int64_t)b->max_len + kPage - 1) / kPage, want = kSplitGrid / base;
+  int64_t part = want > 1 ? (pages + want - 1) / want : pages;
+  const int64_t least = (pages + kMaxSplits - 1) / kMaxSplits;
+  part = part < kWaves ? kWaves : part;
+  part = part < least ? least : part;
+  p.split_pages = (int)part;
+  p.splits = pages > part ? (int)((pages + part - 1) / part) : 1;
   return p;
 }
 
 template <int D>
 const void* attention_kernel(const Plan& p, bool two_terms) {
-  if (p.wave_rows) return two_terms ? (const void*)vbq_kv_attention_kernel<D, 2, true, true> : (const void*)vbq_kv_attention_kernel<D, 2, false, true>;
+  constexpr int NT = wave_tiles(D);
+  if (p.wave_rows) return two_terms ? (const void*)vbq_kv_attention_kernel<D, NT, true, true> : (const void*)vbq_kv_attention_kernel<D, NT, false, true>;
   return two_terms ? (const void*)vbq_kv_attention_kernel<D, 1, true, false> : (const void*)vbq_kv_attention_kernel<D, 1, false, false>;
 }
 
@@ -849,6 +896,7 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc, const vbq_kv
   if (st != VBQ_OK) return st;
   if ((st = check_batch(batch)) != VBQ_OK) return st;
   if (n_q_heads < 1 || n_q_heads % desc->n_heads || n_q_heads / desc->n_heads > VBQ_KV_MAX_GROUP) return VBQ_ERR_SHAPE;
+  if (batch->n_rows * (n_q_heads / desc->n_heads) > (int64_t)1 << 30) return VBQ_ERR_SHAPE;
   *bytes = 0;
   if (batch->n_seqs == 0 || batch->n_rows == 0) return VBQ_OK;
   const Plan p = plan_of(desc, batch, n_q_heads / desc->n_heads);
@@ -877,18 +925,18 @@ vbq_status vbq_kv_attention(const vbq_kv_desc* desc, const void* cache_dev, cons
   const int group = n_q_heads / desc->n_heads;
   const Plan p = plan_of(desc, batch, group);
   AttnArgs a{batch_of(batch), (const uint8_t*)cache_dev, desc->n_pages, desc->n_heads, group, q_type, out_type, q_dev, out_dev,
-             ldq, hsq, ldo, hso, scale, p.tiles, p.splits, (float*)workspace_dev};
+             ldq, hsq, ldo, hso, scale, p.splits, p.split_pages, (float*)workspace_dev};
   void* args[] = {&a};
   const int D = desc->head_dim;
   const bool two = q_type == VBQ_F32;
   const void* f = D == 64 ? attention_kernel<64>(p, two) : D == 128 ? attention_kernel<128>(p, two) : attention_kernel<256>(p, two);
-  const int64_t grid = (int64_t)p.tiles * batch->n_seqs * p.splits * desc->n_heads;
-  if ((st = launch(f, dim3((unsigned)grid), kWaves * 64, args, stream)) != VBQ_OK || p.splits == 1) return st;
+  const dim3 grid((unsigned)(p.splits * desc->n_heads), (unsigned)batch->n_seqs, (unsigned)p.tiles);
+  if ((st = launch(f, grid, kWaves * 64, args, stream)) != VBQ_OK || p.splits == 1) return st;
   const void* j = D == 64    ? (const void*)vbq_kv_join_kernel<64>
                   : D == 128 ? (const void*)vbq_kv_join_kernel<128>
                              : (const void*)vbq_kv_join_kernel<256>;
   const int64_t rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
-  return launch(j, dim3((unsigned)(rows * batch->n_seqs * n_q_heads)), kWaves * 64, args, stream);
+  return launch(j, dim3((unsigned)n_q_heads, (unsigned)batch->n_seqs, (unsigned)(rows < 1024 ? rows : 1024)), kWaves * 64, args, stream);
 }
 
 }  // extern "C"
