@@ -52,11 +52,13 @@ using vbq::value_word;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;           // waves of a workgroup
 constexpr int kMaxSplits = 64;      // parts of a sequence's positions: a lane each in the join
+constexpr int kNowhere = 0x7fffff00; // a position that no row sees
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // ------------------------------------------------------------------ element types
@@ -285,6 +287,12 @@ __device__ __forceinline__ float across_groups(float v, Op op) {
   const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(c, c, false, false));
   return op(__uint_as_float(t[0]), __uint_as_float(t[1]));
 }
+// (fmaxf's operands would each be made quiet first)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float m;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+  return m;
+}
 __device__ __forceinline__ float group_max(float v) {
   return across_groups(v, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
@@ -300,9 +308,10 @@ __device__ __forceinline__ f16x8 code_operand(uint32_t w) {
 }
 
 // Eight codes as the levels u - 8 in fp16: u or 16 u placed in the mantissa of 1024, then one packed
-// operation, all exact.
-__device__ __forceinline__ f16x8 level_operand(uint32_t w) {
-  const uint32_t w8 = w >> 8, one = 0x64006400u;
+// operation, all exact.  `one` is 0x64006400 in a vector register: the AND and the OR are one
+// operation then (of two constants it takes only one from elsewhere).
+__device__ __forceinline__ f16x8 level_operand(uint32_t w, uint32_t one) {
+  const uint32_t w8 = w >> 8;
   const f16x2 unit = {(_Float16)-1032.0f, (_Float16)-1032.0f}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, minus = {(_Float16)-72.0f, (_Float16)-72.0f};
   const f16x2 a = __builtin_bit_cast(f16x2, (w & 0x000f000fu) | one) + unit;
   const f16x2 b = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (w & 0x00f000f0u) | one), sixteenth, minus);
@@ -372,6 +381,7 @@ struct Rows {
   float mu[NT], sum[NT];
   int visible[NT];
   f32x4 o[NT][D / 16];
+  uint32_t one;              // 0x64006400
   int e;                     // E + 21, the fp16 exponent field of the largest value scale
 
   // The row's elements times a power of two that puts the largest into [2^14, 2^15);
@@ -489,24 +499,15 @@ struct Rows {
     }
 
     // ---- the bias moves where a score passes it by 2^8, or a value scale the largest so far
-    uint32_t top = 0;
+    u16x2 tops = __builtin_bit_cast(u16x2, k.vs[0][0]);  // (scales are not negative: their bits order as they do)
 #pragma unroll
-    for (int grp = 0; grp < kGroups; ++grp) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w = k.vs[grp][i], lo = (w >> 10) & 31u, hi = (w >> 26) & 31u;
-        top = top > lo ? top : lo;
-        top = top > hi ? top : hi;
-      }
-    }
+    for (int i = 1; i < 4 * kGroups; ++i) tops = __builtin_elementwise_max(tops, __builtin_bit_cast(u16x2, k.vs[i / 4][i % 4]));
+    const uint32_t top = (uint32_t)(tops.x > tops.y ? tops.x : tops.y) >> 10;
     bool grow = (int)top > e;
     float most[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float m = x[nt][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) m = __builtin_fmaxf(m, x[nt][i]);
-      most[nt] = m * c[nt];
+      most[nt] = max3(max3(max3(x[nt][0], x[nt][1], x[nt][2]), x[nt][3], x[nt][4]), max3(x[nt][5], x[nt][6], x[nt][7]), x[nt][7]) * c[nt];
       grow |= most[nt] > mu[nt] + 8.0f;
     }
     if (__builtin_amdgcn_ballot_w64(grow)) {
@@ -551,7 +552,7 @@ struct Rows {
     }
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
-      const f16x8 vf = level_operand(k.vw[d]);
+      const f16x8 vf = level_operand(k.vw[d], one);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) o[nt][d] = mfma(vf, w[nt][d / 4], o[nt][d]);
     }
@@ -592,12 +593,35 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
     const uint32_t base = tile * kRows + (kWaveRows ? wave * 16 * NT : 0);
     Rows<D, NT, kTwoTerms> r;
     r.e = 0;
+    asm("v_mov_b32 %0, 0x64006400" : "=v"(r.one));
     const uint32_t last = base + 16 * NT < n_rows ? base + 16 * NT : n_rows;
     auto seen = [&](uint32_t row) {
       const int64_t v = s.pos0 + row + 1;
       return (int)(v < 0 ? 0 : v < s.end ? v : s.end);
     };
     const int least = base < n_rows ? seen(base / group) : 0, most = base < n_rows ? seen((last - 1) / group) : 0;
+    const int pages = (most + kPage - 1) / kPage, least_per = (pages + a.splits - 1) / a.splits;
+    const int per = a.split_pages > least_per ? a.split_pages : least_per, step = kWaveRows ? 1 : kWaves;
+    const int64_t first = (int64_t)split * per + (kWaveRows ? 0 : wave);
+    const int stop = (int)(split + 1) * (int64_t)per < pages ? (int)(split + 1) * per : pages;
+    const int64_t heads = (int64_t)a.heads * a.group;
+    if (split && split * (int64_t)per >= pages) {  // nothing to see in this part: the join reads no more of it than that
+      if ((int)threadIdx.x < kRows && tile * kRows + threadIdx.x < n_rows) {
+        const uint32_t i = tile * kRows + threadIdx.x;
+        store_bias<D>(a, (s.row0 + i / group) * heads + hq0 + i % group, (int)split, 0.0f, 0.0f);
+      }
+      continue;
+    }
+    // What is no page of the cache is read as page 0 and hidden.  Ids are read a page ahead, the
+    // first block before the queries.
+    auto id_of = [&](int64_t page) { return page < stop ? page_id(a.batch, a.n_pages, b, page) : -1; };
+    auto load = [&](Block<D>& k, int64_t id, int half) {
+      load_block<D>(k, a.cache + ((id < 0 ? 0 : id) * a.heads + h) * (int64_t)P::kBytes, half, lane);
+    };
+    Block<D> k;
+    int page = (int)(first < stop ? first : stop), half = 0;
+    int64_t id = id_of(first), next = id_of(first + step);
+    if (page < stop) load(k, id, 0);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const uint32_t i = base + 16 * nt + (lane & 15), row = i / group;
@@ -605,27 +629,21 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
       r.visible[nt] = on ? seen(row) : 0;
       r.load(a, nt, s.row0 + (on ? row : 0), hq0 + (on ? i - row * group : 0), g);
     }
-    const int pages = (most + kPage - 1) / kPage, least_per = (pages + a.splits - 1) / a.splits;
-    const int per = a.split_pages > least_per ? a.split_pages : least_per;
-    const int stop = (int)(split + 1) * per < pages ? (int)(split + 1) * per : pages, step = kWaveRows ? 1 : kWaves;
-    int page = (int)split * per + (kWaveRows ? 0 : wave);
-    int64_t next = page < stop ? page_id(a.batch, a.n_pages, b, page) : -1;
-    for (; page < stop; page += step) {
-      const int64_t id = next;
-      if (page + step < stop) next = page_id(a.batch, a.n_pages, b, page + step);
-      if (id < 0) continue;
-      const uint8_t* from = a.cache + (id * a.heads + h) * (int64_t)P::kBytes;
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        const int pos = page * kPage + 32 * half;
-        if (pos >= most) break;
-        Block<D> k;
-        load_block<D>(k, from, half, lane);
-        r.block(k, pos, (int)s.end, g, pos + 32 > least);
+    while (page < stop) {
+      const int pos = id < 0 ? kNowhere : page * kPage + 32 * half;
+      if (half || page * kPage + 32 >= most) {  // the next block is another page's first
+        page += step;
+        id = next;
+        half = 0;
+        next = id_of((int64_t)page + step);
+      } else {
+        half = 1;
       }
+      r.block(k, pos, (int)s.end, g, pos + 32 > least);
+      if (page < stop) load(k, id, half);
     }
 
-    const int64_t heads = (int64_t)a.heads * a.group;
     if constexpr (kWaveRows) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -717,12 +735,6 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
   const int tid = (int)threadIdx.x, side = tid / kLanes, el = 4 * (tid % kLanes);
   for (int64_t i = blockIdx.z; i < s.n; i += gridDim.z) {
     const int64_t rh = (s.row0 + i) * heads + hq;
-    f32x4 part[kTurns];
-#pragma unroll
-    for (int j = 0; j < kTurns; ++j) {
-      const int p = side + j * kSide;
-      part[j] = *(const f32x4*)(a.part + (rh * a.splits + (p < a.splits ? p : 0)) * D + el);
-    }
     float sum = 0.0f;
     if (tid < kMaxSplits) {  // (the first wave)
       const float* pair = a.part + a.batch.n_rows * heads * a.splits * (int64_t)D + 2 * rh * a.splits;
@@ -738,11 +750,18 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
       for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
     }
     __syncthreads();
+    // a part that saw nothing was not written: the first is read in its place, times 0
+    f32x4 part[kTurns];
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+      const int p = side + j * kSide;
+      part[j] = *(const f32x4*)(a.part + (rh * a.splits + (f_lds[p] != 0.0f ? p : 0)) * D + el);
+    }
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < kTurns; ++j) {
       const float f = f_lds[side + j * kSide];
-      if (f != 0.0f) v += part[j] * f;  // (0 also where there is no part)
+      if (f != 0.0f) v += part[j] * f;
     }
     *(f32x4*)&o_lds[side][el] = v;
     __syncthreads();
@@ -759,7 +778,6 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
 // ------------------------------------------------------------------ host side
 
 constexpr int64_t kMaxGrid = (int64_t)1 << 30;
-constexpr int64_t kSplitGrid = 2048;
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
 bool known(int32_t type) { return type == VBQ_F32 || type == VBQ_F16 || type == VBQ_BF16; }
@@ -806,12 +824,15 @@ Plan plan_of(const vbq_kv_desc* d, const vbq_kv_batch* b, int group) {
   p.tiles = (int)(tiles < 16384 ? tiles : 16384);
   if (p.tiles > most) p.tiles = most > 1 ? (int)most : 1;
   // Parts of equal size whatever a sequence's length, so that long sequences of a ragged batch get
-  // more workgroups: up to kSplitGrid if all were max_len long, no part below a page a wave.
-  const int64_t base = units * p.tiles, pages = ((int64_t)b->max_len + kPage - 1) / kPage, want = kSplitGrid / base;
+  // more workgroups: as many as the chip holds at a time if all were max_len long, no part below a page
+  // a wave, nor so small that its sums (4 D bytes a row, written and read) cost a tenth of its pages.
+  const int64_t base = units * p.tiles, pages = ((int64_t)b->max_len + kPage - 1) / kPage;
+  const int64_t want = (p.wave_rows ? 512 : 256 * (d->head_dim == 256 ? 2 : 6)) / base;
   int64_t part = want > 1 ? (pages + want - 1) / want : pages;
-  const int64_t least = (pages + kMaxSplits - 1) / kMaxSplits;
+  const int64_t most_parts = (pages + kMaxSplits - 1) / kMaxSplits, tile_rows = rows < per ? rows : per;
   part = part < kWaves ? kWaves : part;
-  part = part < least ? least : part;
+  part = part < tile_rows ? tile_rows : part;
+  part = part < most_parts ? most_parts : part;
   p.split_pages = (int)part;
   p.splits = pages > part ? (int)((pages + part - 1) / part) : 1;
   return p;
