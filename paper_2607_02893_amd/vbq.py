@@ -7,6 +7,7 @@ module raises on import; there is no fallback.
 """
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -693,33 +694,40 @@ def qat_logit_grad(W, grad, pi, tau, lam, n_bbar=None, dlogits=None, stream=None
 
 # ------------------------------------------ between the products of a decode step
 
+# (A call is often shorter on the GPU than on the host, so the checks below are the cheapest that
+# say the same: one comparison of whole shapes, device numbers instead of device objects, results
+# that the library allocates itself not checked again.)
 if _torch is not None:
     _DTYPES = {_torch.float32: F32, _torch.float16: F16, _torch.bfloat16: BF16}
+    _current_device = _torch.cuda.current_device
+    _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda index: _torch.cuda.current_stream(index).cuda_stream)
 
 
-class _Launch:
-    """The device and stream of a call: tensors allocated inside belong to that
-    stream, so a freed scratch tensor is not handed out while the call runs.
-    `stream` None is the current stream of the tensors' device."""
+class _OtherStream:
+    """A call on another stream or device than the current one: tensors allocated inside belong to
+    that stream, so a freed scratch tensor is not handed out while the call runs."""
 
-    def __init__(self, device, stream):
-        self._undo = None
-        if stream is not None:
-            if stream.device != device:
-                raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-            self._undo = _torch.cuda.stream(stream)
-        elif _torch.cuda.current_device() != device.index:
-            self._undo = _torch.cuda.device(device)
-        self._device = device
+    def __init__(self, index, stream):
+        if stream is not None and stream.device.index != index:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{index}")
+        self._index = index
+        self._context = _torch.cuda.device(index) if stream is None else _torch.cuda.stream(stream)
 
     def __enter__(self):
-        if self._undo is not None:
-            self._undo.__enter__()
-        return _torch.cuda.current_stream(self._device).cuda_stream
+        self._context.__enter__()
+        return _raw_stream(self._index)
 
     def __exit__(self, *exc):
-        if self._undo is not None:
-            self._undo.__exit__(*exc)
+        self._context.__exit__(*exc)
+
+
+def _launch(index, stream, call):
+    """call(raw stream) on `stream`, or on the current stream of device `index`."""
+    if stream is None and _current_device() == index:
+        return call(_raw_stream(index))
+    with _OtherStream(index, stream) as s:
+        return call(s)
 
 
 def _dtype_of(t, name):
@@ -729,24 +737,41 @@ def _dtype_of(t, name):
     return code
 
 
-def _gpu(t, name, device=None):
+def _gpu(t, name):
+    """The device number of a GPU tensor."""
     if t is None or not getattr(t, "is_cuda", False):
         raise ValueError(f"{name} must be a GPU tensor")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
-    return t
+    return t.get_device()
 
 
-def _rows(t, name, shape, device=None):
-    """A GPU tensor of this shape whose last dimension is contiguous."""
-    _gpu(t, name, device)
-    if tuple(t.shape) != tuple(shape) or (t.stride(-1) != 1 and t.shape[-1] != 1):
+def _rows(t, name, shape, index):
+    """A tensor on device `index`, of this shape, whose last dimension is contiguous."""
+    if _gpu(t, name) != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if t.shape != shape or (t.stride(-1) != 1 and shape[-1] != 1):
         raise ValueError(f"{name} must be a {list(shape)} tensor with unit stride in the last dimension")
     return t
 
 
+def _vector(t, name, dtype, n, index):
+    """A contiguous one-dimensional tensor on device `index`."""
+    if _gpu(t, name) != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _scratch(t, index):
+    if _gpu(t, "workspace") != index or t.dtype != _torch.uint8 or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{index}")
+    return t.data_ptr()
+
+
 def _spread(t, name):
     """A tensor that is written: no two of its elements share memory."""
+    if t.is_contiguous():
+        return t
     reach = 1
     for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n > 1):
         if stride < reach:
@@ -763,44 +788,49 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
     weight: contiguous [K] or None.  h: a tensor to write the sum into (residual
     itself for in place); None allocates it, False leaves it out.  x is x_dtype (float16, the products' input).
     Returns (x, h), h None where left out (and residual itself where y is None and no h is given)."""
-    _gpu(residual, "residual")
-    dev, K = residual.device, residual.shape[-1]
+    index = _gpu(residual, "residual")
     shape = residual.shape
+    if not shape or not shape[-1]:
+        raise ValueError("residual must be [..., K] with K >= 1")
+    K = shape[-1]
+    n = residual.numel() // K
     two = len(shape) == 2
-    if x_dtype is None:
-        x_dtype = _torch.float16 if x is None else x.dtype
-    if not two:
-        for t, name in ((residual, "residual"), (y, "y"), (x, "x"), (h if h is not False else None, "h")):
-            if t is not None and not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous unless it has two dimensions")
-    for t, name in ((residual, "residual"), (y, "y")):
-        if t is not None:
-            _rows(t, name, shape, dev)
+
+    def row(t, name):
+        if t.is_contiguous():
+            return K
+        if not two:
+            raise ValueError(f"{name} must be contiguous unless it has two dimensions")
+        return t.stride(0) if n > 1 else K
+
+    r_type, r_row = _dtype_of(_rows(residual, "residual", shape, index), "residual"), row(residual, "residual")
+    y_ptr = y_type = y_row = w_ptr = w_type = h_ptr = h_row = 0
+    if y is not None:
+        y_type, y_row, y_ptr = _dtype_of(_rows(y, "y", shape, index), "y"), row(y, "y"), y.data_ptr()
     if weight is not None:
-        _rows(weight, "weight", (K,), dev)
-    with _Launch(dev, stream) as s:
-        if x is None:
-            x = _torch.empty(shape, dtype=x_dtype, device=dev)
-        if h is None:
-            h = residual if y is None else _torch.empty(shape, dtype=residual.dtype, device=dev)
-        _spread(_rows(x, "x", shape, dev), "x")
-        if h is not False and h is not residual:
-            _spread(_rows(h, "h", shape, dev), "h")
-            if h.dtype != residual.dtype:
-                raise ValueError("h must have residual's type")
-        if x.dtype != x_dtype:
+        w_type, w_ptr = _dtype_of(_rows(weight, "weight", (K,), index), "weight"), weight.data_ptr()
+    if x is not None:
+        _spread(_rows(x, "x", shape, index), "x")
+        if x_dtype is not None and x.dtype != x_dtype:
             raise ValueError(f"x must be {x_dtype}")
-        n = residual.numel() // K if K else 0
-        row = lambda t: (t.stride(0) if two and n > 1 else K)  # noqa: E731
-        keep = None if h is False or (h is residual and y is None) else h
-        if keep is residual:
-            _spread(residual, "residual")
-        _check(_lib.vbq_add_norm(n, K, _dtype_of(residual, "residual"), residual.data_ptr(), row(residual),
-                                 0 if y is None else _dtype_of(y, "y"), None if y is None else y.data_ptr(),
-                                 0 if y is None else row(y), 0 if weight is None else _dtype_of(weight, "weight"),
-                                 None if weight is None else weight.data_ptr(), eps,
-                                 None if keep is None else keep.data_ptr(), 0 if keep is None else row(keep),
-                                 _dtype_of(x, "x"), x.data_ptr(), row(x), s), "vbq_add_norm")
+    given = h is not None and h is not False
+    if given:
+        _spread(_rows(h, "h", shape, index), "h")
+        if h.dtype != residual.dtype:
+            raise ValueError("h must have residual's type")
+
+    def call(s):
+        nonlocal x, h, h_ptr, h_row
+        if x is None:
+            x = _torch.empty(shape, dtype=x_dtype or _torch.float16, device=residual.device)
+        if h is None:
+            h = residual if y is None else _torch.empty(shape, dtype=residual.dtype, device=residual.device)
+        if h is not False and (h is not residual or y is not None):
+            h_ptr, h_row = h.data_ptr(), row(h, "h")
+        return _lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), r_row, y_type, y_ptr or None, y_row, w_type, w_ptr or None, eps,
+                                 h_ptr or None, h_row, _dtype_of(x, "x"), x.data_ptr(), row(x, "x"), s)
+
+    _check(_launch(index, stream, call), "vbq_add_norm")
     return x, (None if h is False else h)
 
 
@@ -817,26 +847,29 @@ class KVBatch:
     (a captured graph reads them anew); they must stay alive until the call has run."""
 
     def __init__(self, page_table, seq_len, rows=None, n_rows=None, max_rows=1, max_len=None):
-        dev = _gpu(page_table, "page_table").device
+        self.index = _gpu(page_table, "page_table")
         if page_table.dim() != 2 or seq_len is None or seq_len.dim() != 1 or page_table.shape[0] != seq_len.shape[0]:
             raise ValueError("page_table must be [n_seqs, pages] and seq_len [n_seqs]")
         n, pages = page_table.shape
-        _need(page_table, "page_table", _torch.int32)
-        _need(seq_len, "seq_len", _torch.int32, n, dev)
+        _vector(page_table, "page_table", _torch.int32, n * pages, self.index)
+        _vector(seq_len, "seq_len", _torch.int32, n, self.index)
         if rows is not None:
-            _need(rows, "rows", _torch.int32, n + 1, dev)
+            _vector(rows, "rows", _torch.int32, n + 1, self.index)
             if n_rows is None:
                 raise ValueError("rows needs n_rows")
-        self.device, self.n_seqs, self.max_rows = dev, n, int(max_rows)
+        self.n_seqs, self.max_rows = n, int(max_rows)
         self.n_rows = n * self.max_rows if n_rows is None else int(n_rows)
         self.page_table, self.seq_len, self.rows = page_table, seq_len, rows
         self.max_len = min(pages * KV_PAGE, 2 ** 31 - 1) if max_len is None else int(max_len)
         for name in ("n_rows", "max_rows", "max_len"):
             if not 0 <= getattr(self, name) < 2 ** 31:
                 raise ValueError(f"{name} must be in [0, 2^31)")
+        if pages >= 2 ** 31:
+            raise ValueError("page_table has too many pages")
         self.c = VbqKvBatch(n, pages, page_table.data_ptr(), None if rows is None else rows.data_ptr(),
                             seq_len.data_ptr(), self.n_rows, self.max_rows, self.max_len)
         self._ref = ctypes.byref(self.c)
+        self._workspace = {}  # bytes by cache and query heads: functions of the fields above
 
 
 class KVCache:
@@ -850,79 +883,109 @@ class KVCache:
         self.data = _torch.zeros(self.desc.total_bytes, dtype=_torch.uint8, device=device)
         if self.data.data_ptr() % 256:
             raise VbqError(7, "KVCache")
+        self.index = _gpu(self.data, "the cache")
         self._ref = ctypes.byref(self.desc)
 
     @property
     def nbytes(self):
         return int(self.desc.total_bytes)
 
-    def _of_rows(self, t, name, batch, heads, dtype=None):
-        _rows(t, name, (batch.n_rows, heads, self.head_dim), self.data.device)
-        if dtype is not None and t.dtype != dtype:
-            raise ValueError(f"{name} must be {dtype}")
-        return t
+    def _of_rows(self, t, name, batch, heads):
+        """(address, row stride, head stride) of rows [n_rows, heads, head_dim]; a dimension of one
+        element has no stride that counts."""
+        shape = (batch.n_rows, heads, self.head_dim)
+        if t.shape == shape and t.is_contiguous() and t.is_cuda and t.get_device() == self.index:
+            return t.data_ptr(), heads * self.head_dim, self.head_dim
+        _rows(t, name, shape, self.index)
+        return (t.data_ptr(), t.stride(0) if shape[0] > 1 else heads * self.head_dim,
+                t.stride(1) if heads > 1 else self.head_dim)
 
     def _batch(self, batch):
-        if batch.device != self.data.device:
-            raise ValueError(f"the batch is on {batch.device}, the cache on {self.data.device}")
+        if batch.index != self.index:
+            raise ValueError(f"the batch is on cuda:{batch.index}, the cache on cuda:{self.index}")
         return batch._ref
 
     def append(self, k, v, batch, stream=None):
         """Quantizes rows k, v [n_rows, n_heads, head_dim] (one type; views such as the columns of a fused
         projection's y will do: strides multiples of 8, 16-byte aligned) into the cache (vbq_kv_append)."""
-        self._of_rows(k, "k", batch, self.n_heads)
-        self._of_rows(v, "v", batch, self.n_heads, k.dtype)
         ref = self._batch(batch)
-        with _Launch(self.data.device, stream) as s:
-            _check(_lib.vbq_kv_append(self._ref, self.data.data_ptr(), ref, _dtype_of(k, "k"), k.data_ptr(), k.stride(0),
-                                      k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), s), "vbq_kv_append")
+        _gpu(k, "k"), _gpu(v, "v")
+        k_ptr, ldk, hsk = self._of_rows(k, "k", batch, self.n_heads)
+        v_ptr, ldv, hsv = self._of_rows(v, "v", batch, self.n_heads)
+        if k.dtype != v.dtype:
+            raise ValueError("k and v must be of one type")
+        data, t = self.data.data_ptr(), _dtype_of(k, "k")
+        _check(_launch(self.index, stream, lambda s: _lib.vbq_kv_append(self._ref, data, ref, t, k_ptr, ldk, hsk, v_ptr, ldv, hsv, s)),
+               "vbq_kv_append")
 
     def dequant(self, batch, k=None, v=None, stream=None):
         """(k, v), float32 [n_rows, n_heads, head_dim]: the values the cache holds at the
         positions of the call's rows (vbq_kv_dequant); rows without a place are left as they are (zeros where allocated here)."""
-        dev, shape, ref = self.data.device, (batch.n_rows, self.n_heads, self.head_dim), self._batch(batch)
-        with _Launch(dev, stream) as s:
-            k = _torch.zeros(shape, dtype=_torch.float32, device=dev) if k is None else k
-            v = _torch.zeros(shape, dtype=_torch.float32, device=dev) if v is None else v
-            for t, name in ((k, "k"), (v, "v")):
-                _need(self._of_rows(t, name, batch, self.n_heads), name, _torch.float32)
-            _check(_lib.vbq_kv_dequant(self._ref, self.data.data_ptr(), ref, k.data_ptr(), v.data_ptr(), s), "vbq_kv_dequant")
+        ref, shape = self._batch(batch), (batch.n_rows, self.n_heads, self.head_dim)
+        for t, name in ((k, "k"), (v, "v")):
+            if t is not None and (_rows(t, name, shape, self.index).dtype != _torch.float32 or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous float32")
+
+        def call(s):
+            nonlocal k, v
+            if k is None:
+                k = _torch.zeros(shape, dtype=_torch.float32, device=self.data.device)
+            if v is None:
+                v = _torch.zeros(shape, dtype=_torch.float32, device=self.data.device)
+            return _lib.vbq_kv_dequant(self._ref, self.data.data_ptr(), ref, k.data_ptr(), v.data_ptr(), s)
+
+        _check(_launch(self.index, stream, call), "vbq_kv_dequant")
         return k, v
 
     def attention_workspace_size(self, batch, n_q_heads):
-        nbytes = ctypes.c_size_t(0)
-        _check(_lib.vbq_kv_attention_workspace_size(self._ref, batch._ref, n_q_heads, ctypes.byref(nbytes)),
-               "vbq_kv_attention_workspace_size")
-        return nbytes.value
+        key = (self.n_heads, self.head_dim, n_q_heads)
+        if key not in batch._workspace:
+            nbytes = ctypes.c_size_t(0)
+            _check(_lib.vbq_kv_attention_workspace_size(self._ref, batch._ref, n_q_heads, ctypes.byref(nbytes)),
+                   "vbq_kv_attention_workspace_size")
+            batch._workspace[key] = nbytes.value
+        return batch._workspace[key]
 
     def attention(self, q, batch, scale=None, out=None, out_dtype=None, workspace=None, stream=None):
         """Attention of q [n_rows, n_q_heads, head_dim] over the cache (vbq_kv_attention): each row
         sees its sequence's positions up to its own.  scale: 1/sqrt(head_dim) by default.  out: q's type, or
         out_dtype; rows of no sequence are left as they are (uninitialised where out is allocated here).
         workspace: uint8 tensor of attention_workspace_size bytes, allocated where not given."""
-        dev, ref = self.data.device, self._batch(batch)
-        heads = q.shape[1] if getattr(q, "dim", lambda: 0)() == 3 else 0
-        self._of_rows(q, "q", batch, heads)
-        if out_dtype is None:
-            out_dtype = q.dtype if out is None else out.dtype
-        with _Launch(dev, stream) as s:
+        ref = self._batch(batch)
+        _gpu(q, "q")
+        if q.dim() != 3:
+            raise ValueError("q must be [n_rows, n_q_heads, head_dim]")
+        heads = q.shape[1]
+        q_ptr, ldq, hsq = self._of_rows(q, "q", batch, heads)
+        q_type = _dtype_of(q, "q")
+        if out is not None:
+            _gpu(out, "out")
+            if out_dtype is not None and out.dtype != out_dtype:
+                raise ValueError(f"out must be {out_dtype}")
+            _spread(out, "out")
+        need = self.attention_workspace_size(batch, heads)
+        given = None if workspace is None else (_scratch(workspace, self.index), workspace.numel())
+
+        def call(s):
+            nonlocal out
             if out is None:
-                out = _torch.empty(q.shape, dtype=out_dtype, device=dev)
-            _spread(self._of_rows(out, "out", batch, heads, out_dtype), "out")
-            need = self.attention_workspace_size(batch, heads)
-            if workspace is None and need:
-                workspace = _torch.empty(need, dtype=_torch.uint8, device=dev)
-            elif workspace is not None:
-                _need(workspace, "workspace", _torch.uint8, None, dev)
-            _check(_lib.vbq_kv_attention(self._ref, self.data.data_ptr(), ref, heads,
-                                         self.head_dim ** -0.5 if scale is None else scale, _dtype_of(q, "q"), q.data_ptr(),
-                                         q.stride(0), q.stride(1), _dtype_of(out, "out"), out.data_ptr(), out.stride(0),
-                                         out.stride(1), None if workspace is None else workspace.data_ptr(),
-                                         0 if workspace is None else workspace.numel(), s), "vbq_kv_attention")
+                out = _torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+            o_ptr, ldo, hso = self._of_rows(out, "out", batch, heads)
+            ws, n = given or (0, 0)
+            if need and not given:
+                scratch = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+                ws, n = scratch.data_ptr(), need
+            return _lib.vbq_kv_attention(self._ref, self.data.data_ptr(), ref, heads,
+                                         self.head_dim ** -0.5 if scale is None else scale, q_type, q_ptr, ldq, hsq,
+                                         _dtype_of(out, "out"), o_ptr, ldo, hso, ws or None, n, s)
+
+        _check(_launch(self.index, stream, call), "vbq_kv_attention")
         return out
 
 
+@functools.lru_cache(maxsize=256)
 def sample_workspace_size(M, V):
+    """Bytes of device scratch that sample() takes for M rows of V logits."""
     nbytes = ctypes.c_size_t(0)
     _check(_lib.vbq_sample_workspace_size(M, V, ctypes.byref(nbytes)), "vbq_sample_workspace_size")
     return nbytes.value
@@ -933,36 +996,41 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
     """One token a row (vbq_sample): logits [M, V] (rows may be padded), u float32 [M] the
     random numbers in [0, 1), temperature / top_p / min_p float32 [M] and top_k int32 [M] device tensors or None.
     probs: a tensor to write into, None to allocate, False to leave out.  Returns (tokens int32 [M], probs float32 [M] or None)."""
-    _gpu(logits, "logits")
-    dev = logits.device
+    index = _gpu(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be [M, V]")
     M, V = logits.shape
-    _rows(logits, "logits", (M, V), dev)
-    _need(u, "u", _torch.float32, M, dev)
-    for t, name, dtype in ((temperature, "temperature", _torch.float32), (top_k, "top_k", _torch.int32),
-                           (top_p, "top_p", _torch.float32), (min_p, "min_p", _torch.float32)):
-        if t is not None:
-            _need(t, name, dtype, M, dev)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    with _Launch(dev, stream) as s:
+    f32, i32 = _torch.float32, _torch.int32
+    if logits.stride(1) != 1 and V > 1:
+        raise ValueError("logits must have unit stride in the last dimension")
+    u_ptr = _vector(u, "u", f32, M, index)
+    t_ptr = None if temperature is None else _vector(temperature, "temperature", f32, M, index)
+    k_ptr = None if top_k is None else _vector(top_k, "top_k", i32, M, index)
+    p_ptr = None if top_p is None else _vector(top_p, "top_p", f32, M, index)
+    m_ptr = None if min_p is None else _vector(min_p, "min_p", f32, M, index)
+    if tokens is not None:
+        _vector(tokens, "tokens", i32, M, index)
+    if probs is not None and probs is not False:
+        _vector(probs, "probs", f32, M, index)
+    need = sample_workspace_size(M, V)
+    given = None if workspace is None else (_scratch(workspace, index), workspace.numel())
+
+    def call(s):
+        nonlocal tokens, probs
+        dev = logits.device
         if tokens is None:
-            tokens = _torch.empty(M, dtype=_torch.int32, device=dev)
+            tokens = _torch.empty(M, dtype=i32, device=dev)
         if probs is None:
-            probs = _torch.empty(M, dtype=_torch.float32, device=dev)
-        probs = None if probs is False else probs
-        _need(tokens, "tokens", _torch.int32, M, dev)
-        if probs is not None:
-            _need(probs, "probs", _torch.float32, M, dev)
-        need = sample_workspace_size(M, V)
-        if workspace is None and need:
-            workspace = _torch.empty(need, dtype=_torch.uint8, device=dev)
-        elif workspace is not None:
-            _need(workspace, "workspace", _torch.uint8, None, dev)
-        _check(_lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V,
-                               ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p), u.data_ptr(), tokens.data_ptr(),
-                               ptr(probs), ptr(workspace), 0 if workspace is None else workspace.numel(), s), "vbq_sample")
-    return tokens, probs
+            probs = _torch.empty(M, dtype=f32, device=dev)
+        ws, n = given or (0, 0)
+        if need and not given:
+            scratch = _torch.empty(need, dtype=_torch.uint8, device=dev)
+            ws, n = scratch.data_ptr(), need
+        return _lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V, t_ptr, k_ptr,
+                               p_ptr, m_ptr, u_ptr, tokens.data_ptr(), None if probs is False else probs.data_ptr(), ws or None, n, s)
+
+    _check(_launch(index, stream, call), "vbq_sample")
+    return tokens, (None if probs is False else probs)
 
 
 def raw_qat_logit_grad(n_groups, W_ptr, grad_ptr, pi_ptr, tau, lam, n_bbar, d_ptr, stream_ptr):
