@@ -377,8 +377,8 @@ struct Rows {
   static constexpr int kGroups = D / 64;
   f16x8 q[NT][D / 32], q_low[kTwoTerms ? NT : 1][D / 32];
   float start[NT][kGroups];  // -8 2^-24 sum of q over a group
-  float c[NT];               // what a raw score is multiplied with to be a power of two
-  float mu[NT], sum[NT];
+  f32x4 c;                   // (by tile) what a raw score is multiplied with to be a power of two
+  f32x4 mu, sum;             // (vectors: as arrays these three were kept in LDS, three accesses a block)
   int visible[NT];
   f32x4 o[NT][D / 16];
   uint32_t one;              // 0x64006400

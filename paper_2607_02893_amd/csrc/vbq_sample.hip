@@ -37,6 +37,8 @@ vbq_status vbq_detail_hip_status(hipError_t e);
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kThreads = 1024;
 constexpr int kWavesRow = kThreads / 64;  // 16: a value a wave is a row of lanes
 constexpr double kOne = 0x1p43;  // the weight of the largest logit; 2^20 of them stay below 2^63
@@ -45,6 +47,7 @@ constexpr double kNone = -1e300;
 constexpr int kBinsPerUnit = 16, kBins = 489;  // (the last holds x = kLeast alone)
 constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;  // of a key, at a time
 constexpr int kCap = 4096;       // entries of a list; rows up to this length take one workgroup
+constexpr int kRanked = kThreads / 4;  // entries of a list that is ordered pair by pair
 constexpr int kMaxChunks = 32;
 constexpr int64_t kRowsAtOnce = 64;   // rows of a set of launches: bounds the workspace
 
@@ -627,6 +630,7 @@ __global__ __launch_bounds__(kThreads) void vbq_sample_token_kernel(LongArgs a) 
   __shared__ Cuts cuts;
   __shared__ uint32_t keys[kCap], index[kCap];
   __shared__ uint16_t bins[kCap];
+  __shared__ __attribute__((aligned(16))) u32x4 entries[kRanked];  // key, bin and index, weight
   __shared__ uint64_t whole[kCap];
   __shared__ uint64_t chunk_w[kMaxChunks];
   __shared__ uint64_t before_chunk, the_total;
@@ -654,6 +658,7 @@ __global__ __launch_bounds__(kThreads) void vbq_sample_token_kernel(LongArgs a) 
     index[i] = (uint32_t)v;
     bins[i] = (uint16_t)w.bin(keys[i]);
     whole[i] = w.whole(keys[i]);
+    if (i < kRanked) entries[i] = u32x4{keys[i], ((uint32_t)bins[i] << 20) | index[i], (uint32_t)whole[i], (uint32_t)(whole[i] >> 32)};
   }
   if (tid < kMaxChunks) chunk_w[tid] = tid < a.chunks ? st.sum[tid] : 0;
   __syncthreads();
@@ -661,28 +666,60 @@ __global__ __launch_bounds__(kThreads) void vbq_sample_token_kernel(LongArgs a) 
   Cut cut = {0, 0, true};
   uint64_t kept = c.all_w;
   uint32_t last_tie = 0xffffffffu;  // of the cut's equals those up to this index are kept
-#pragma unroll 1  // one copy of the steps' code: a workgroup alone waits for its instructions too
-  for (int step = 0; step < 3; ++step) {  // top-k, top-p, which of the cut's equals
-    if (step == 0 ? c.k_bin < 0 : step == 1 ? c.p_lo < 0 : cut.all) continue;
-    const int lo = step == 0 ? c.k_bin : c.p_lo, hi = step == 0 ? c.k_bin : c.p_hi;
-    const Cut got = cut_keys(
-        bl, n,
-        [&](int i) {
-          if (step == 2) return keys[i] == cut.key ? ~index[i] : 0u;
-          return bins[i] >= lo && bins[i] <= hi ? keys[i] : 0u;
-        },
-        [&](int i) { return whole[i]; }, w, step != 1, step == 0 ? (uint64_t)l.k : cut.take,
-        target_within((double)l.p * (double)kept, kept), step == 1 ? c.p_above_w : 0, step == 0 ? c.k_above_c : 0);
-    if (step == 2) {
-      last_tie = ~got.key;
-      break;
+  if (n > 0 && n <= kRanked) {
+    // A short list is ordered by comparing every entry with every other, four threads an
+    // entry: two barriers, where the digits take nine a limit.  The last entry kept is the cut.
+    const int i = tid >> 2;
+    const uint32_t key = i < n ? keys[i] : 0, at = i < n ? index[i] : 0;
+    const int bin = i < n ? bins[i] : kBins;
+    uint32_t rank = 0;
+    uint64_t before = 0;
+    if (i < n) {
+#pragma unroll 4
+      for (int j = tid & 3; j < n; j += 4) {
+        const u32x4 e = entries[j];
+        const int other = (int)(e.y >> 20);
+        const bool first = e.x > key || (e.x == key && (e.y & 0xfffffu) < at);
+        rank += first && other == c.k_bin;
+        before += first && other >= c.p_lo && other <= c.p_hi ? ((uint64_t)e.w << 32) | e.z : 0;
+      }
     }
-    cut = shorter(got, cut);
-    if (step == 0 && c.p_lo >= 0) {
-      uint64_t above = 0;
+    rank += from_lane<0xB1, 0xf>(rank);  // (the four threads' sums: from the neighbour, then from the other pair)
+    rank += from_lane<0x4E, 0xf>(rank);
+    before += from_lane<0xB1, 0xf>(before);
+    before += from_lane<0x4E, 0xf>(before);
+    const bool by_k = c.k_bin < 0 || bin < c.k_bin || (bin == c.k_bin && c.k_above_c + rank < (uint64_t)l.k);
+    if (c.k_bin >= 0 && c.p_lo >= 0)
+      kept = c.k_above_w + bl.sum((tid & 3) == 0 && bin == c.k_bin && by_k ? whole[i] : 0);
+    const double target = target_within((double)l.p * (double)kept, kept);
+    const bool by_p = c.p_lo < 0 || bin < c.p_lo || (bin <= c.p_hi && (double)(c.p_above_w + before) < target);
+    const uint64_t last = bl.most(i < n && by_k && by_p ? ((uint64_t)~key << 32) | at : 0);
+    cut.key = ~(uint32_t)(last >> 32);
+    last_tie = (uint32_t)last;
+  } else {
+#pragma unroll 1  // one copy of the steps' code: a workgroup alone waits for its instructions too
+    for (int step = 0; step < 3; ++step) {  // top-k, top-p, which of the cut's equals
+      if (step == 0 ? c.k_bin < 0 : step == 1 ? c.p_lo < 0 : cut.all) continue;
+      const int lo = step == 0 ? c.k_bin : c.p_lo, hi = step == 0 ? c.k_bin : c.p_hi;
+      const Cut got = cut_keys(
+          bl, n,
+          [&](int i) {
+            if (step == 2) return keys[i] == cut.key ? ~index[i] : 0u;
+            return bins[i] >= lo && bins[i] <= hi ? keys[i] : 0u;
+          },
+          [&](int i) { return whole[i]; }, w, step != 1, step == 0 ? (uint64_t)l.k : cut.take,
+          target_within((double)l.p * (double)kept, kept), step == 1 ? c.p_above_w : 0, step == 0 ? c.k_above_c : 0);
+      if (step == 2) {
+        last_tie = ~got.key;
+        break;
+      }
+      cut = shorter(got, cut);
+      if (step == 0 && c.p_lo >= 0) {
+        uint64_t above = 0;
 #pragma unroll 1
-      for (int i = tid; i < n; i += kThreads) above += bins[i] == c.k_bin && keys[i] > cut.key ? whole[i] : 0;
-      kept = c.k_above_w + bl.sum(above) + cut.take * w.whole(cut.key);
+        for (int i = tid; i < n; i += kThreads) above += bins[i] == c.k_bin && keys[i] > cut.key ? whole[i] : 0;
+        kept = c.k_above_w + bl.sum(above) + cut.take * w.whole(cut.key);
+      }
     }
   }
 #pragma unroll 1
@@ -708,32 +745,42 @@ __global__ __launch_bounds__(kThreads) void vbq_sample_token_kernel(LongArgs a) 
   __syncthreads();
   const uint64_t total = the_total;
   const double want = wanted(l.u, total);
-  // the chunk's elements again, each thread a run of them
-  auto own_at = [&](int i) -> uint64_t {
-    const uint32_t key = key_at(a.s, row, i);
-    if (key == 0 || key < cut.key) return 0;
-    if (key == cut.key && (uint32_t)i > last_tie) return 0;
-    return w.kept(key, l.least);
-  };
+  // the chunk's elements again, each thread a run of them, kAhead loads at a time
   const int first = the_chunk * a.per, end = first + a.per < a.s.V ? first + a.per : a.s.V;
   const int each = (a.per + kThreads - 1) / kThreads, lo = first + tid * each, hi = lo + each < end ? lo + each : end;
+  auto own_of = [&](int i, uint32_t key) -> uint64_t {
+    return key == 0 || key < cut.key || (key == cut.key && (uint32_t)i > last_tie) ? 0 : w.kept(key, l.least);
+  };
+  auto load_run = [&](int i, uint32_t (&key)[kAhead]) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) key[j] = i + j < hi ? key_at(a.s, row, i + j) : 0;
+  };
   uint64_t part = 0;
 #pragma unroll 1
-  for (int i = lo; i < hi; ++i) part += own_at(i);
+  for (int i = lo; i < hi; i += kAhead) {
+    uint32_t key[kAhead];
+    load_run(i, key);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) part += own_of(i + j, key[j]);
+  }
   uint64_t run = before_chunk + bl.before(part);
   if (part == 0 || (double)run > want || !((double)(run + part) > want)) return;
 #pragma unroll 1
-  for (int i = lo; i < hi; ++i) {
-    const uint64_t own = own_at(i);
-    run += own;
-    if (own && (double)run > want) {
-      write_token(a.s, row, i, (float)((double)own / (double)total));
-      return;
+  for (int i = lo; i < hi; i += kAhead) {
+    uint32_t key[kAhead];
+    load_run(i, key);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const uint64_t own = own_of(i + j, key[j]);
+      if (own && !((double)run > want) && (double)(run + own) > want)
+        write_token(a.s, row, i + j, (float)((double)own / (double)total));
+      run += own;
     }
   }
 }
 
-// Chunks of a long row: enough workgroups for the chip over all rows, none below 1024 logits.
+// Chunks of a long row: a workgroup a CU over all rows (two took 57 us for 16 rows of 128256, one 49:
+// each finds the cuts for itself), none below 1024 logits.
 void split_row(int64_t M, int64_t V, int32_t* chunks, int32_t* per) {
   const int64_t rows = M < kRowsAtOnce ? M : kRowsAtOnce;
   int64_t c = (256 + rows - 1) / rows;

@@ -794,17 +794,17 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
         raise ValueError("residual must be [..., K] with K >= 1")
     K = shape[-1]
     n = residual.numel() // K
-    two = len(shape) == 2
 
     def row(t, name):
         if t.is_contiguous():
             return K
-        if not two:
+        if len(shape) != 2:
             raise ValueError(f"{name} must be contiguous unless it has two dimensions")
         return t.stride(0) if n > 1 else K
 
-    r_type, r_row = _dtype_of(_rows(residual, "residual", shape, index), "residual"), row(residual, "residual")
-    y_ptr = y_type = y_row = w_ptr = w_type = h_ptr = h_row = 0
+    r_type = _dtype_of(_rows(residual, "residual", shape, index), "residual")
+    y_ptr = w_ptr = h_ptr = None
+    y_type = y_row = w_type = h_row = 0
     if y is not None:
         y_type, y_row, y_ptr = _dtype_of(_rows(y, "y", shape, index), "y"), row(y, "y"), y.data_ptr()
     if weight is not None:
@@ -813,8 +813,7 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
         _spread(_rows(x, "x", shape, index), "x")
         if x_dtype is not None and x.dtype != x_dtype:
             raise ValueError(f"x must be {x_dtype}")
-    given = h is not None and h is not False
-    if given:
+    if h is not None and h is not False:
         _spread(_rows(h, "h", shape, index), "h")
         if h.dtype != residual.dtype:
             raise ValueError("h must have residual's type")
@@ -827,8 +826,8 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
             h = residual if y is None else _torch.empty(shape, dtype=residual.dtype, device=residual.device)
         if h is not False and (h is not residual or y is not None):
             h_ptr, h_row = h.data_ptr(), row(h, "h")
-        return _lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), r_row, y_type, y_ptr or None, y_row, w_type, w_ptr or None, eps,
-                                 h_ptr or None, h_row, _dtype_of(x, "x"), x.data_ptr(), row(x, "x"), s)
+        return _lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), row(residual, "residual"), y_type, y_ptr, y_row, w_type, w_ptr, eps,
+                                 h_ptr, h_row, _dtype_of(x, "x"), x.data_ptr(), row(x, "x"), s)
 
     _check(_launch(index, stream, call), "vbq_add_norm")
     return x, (None if h is False else h)
@@ -920,7 +919,8 @@ class KVCache:
 
     def dequant(self, batch, k=None, v=None, stream=None):
         """(k, v), float32 [n_rows, n_heads, head_dim]: the values the cache holds at the
-        positions of the call's rows (vbq_kv_dequant); rows without a place are left as they are (zeros where allocated here)."""
+        positions of the call's rows (vbq_kv_dequant); rows without a place are left as they are
+        (uninitialised where allocated here)."""
         ref, shape = self._batch(batch), (batch.n_rows, self.n_heads, self.head_dim)
         for t, name in ((k, "k"), (v, "v")):
             if t is not None and (_rows(t, name, shape, self.index).dtype != _torch.float32 or not t.is_contiguous()):
@@ -929,9 +929,9 @@ class KVCache:
         def call(s):
             nonlocal k, v
             if k is None:
-                k = _torch.zeros(shape, dtype=_torch.float32, device=self.data.device)
+                k = _torch.empty(shape, dtype=_torch.float32, device=self.data.device)
             if v is None:
-                v = _torch.zeros(shape, dtype=_torch.float32, device=self.data.device)
+                v = _torch.empty(shape, dtype=_torch.float32, device=self.data.device)
             return _lib.vbq_kv_dequant(self._ref, self.data.data_ptr(), ref, k.data_ptr(), v.data_ptr(), s)
 
         _check(_launch(self.index, stream, call), "vbq_kv_dequant")
