@@ -174,42 +174,61 @@ __global__ __launch_bounds__(256) void vbq_kv_append_kernel(AppendArgs a) {
     const int64_t pos = block * 32 + t;
     const bool on = pos >= first && pos < s.end;
     const int64_t row = s.row0 + (on ? pos - s.pos0 : 0);
+    // every load goes out before the first is used: a token's append is a chain of latencies
+    float fk[P::kGroups][8], fv[P::kGroups][8];
 #pragma unroll
     for (int grp = 0; grp < P::kGroups; ++grp) {
-      const int d = 64 * grp + 8 * sub, slot = slot_of(t);
-      float f[8] = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) fk[grp][i] = fv[grp][i] = 0.0f;
+    }
+    if (on) {
+#pragma unroll
+      for (int grp = 0; grp < P::kGroups; ++grp) {
+        load8(a.k, row * a.ldk + h * a.hsk + 64 * grp + 8 * sub, a.type, fk[grp]);
+        load8(a.v, row * a.ldv + h * a.hsv + 64 * grp + 8 * sub, a.type, fv[grp]);
+      }
+    }
+    constexpr int kWords = D * 4 / 256;  // value words of a thread
+    uint32_t mask[kWords], old[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const int at = tid + 256 * i, d = at >> 2, g = at & 3;
+      mask[i] = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int64_t p = block * 32 + 4 * g + (k & 3) + 16 * (k >> 2);
+        if (p >= first && p < s.end) mask[i] |= 15u << code_bit(k);
+      }
+      old[i] = 0;
+      if (mask[i] && ~mask[i]) old[i] = *(const uint32_t*)(page + value_word<D>(half, d, g));
+    }
+    const int slot = slot_of(t);
+#pragma unroll
+    for (int grp = 0; grp < P::kGroups; ++grp) {
+      const int d = 64 * grp + 8 * sub;
       int c[8];
-      if (on) load8(a.k, row * a.ldk + h * a.hsk + d, a.type, f);
-      const float ks = quantize8(f, c);
+      const float ks = quantize8(fk[grp], c);
       if (on) {
         uint32_t w = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w |= (uint32_t)c[i] << code_bit(i);
         *(uint32_t*)(page + key_word<D>(32 * half + t, d >> 5, (d >> 3) & 3)) = w;
         if (sub == 0) *(_Float16*)(page + P::kKeyScales + 128 * grp + 2 * (32 * half + slot)) = (_Float16)ks;
-        load8(a.v, row * a.ldv + h * a.hsv + d, a.type, f);
       }
-      const float vs = quantize8(f, c);
+      const float vs = quantize8(fv[grp], c);
       if (on && sub == 0) *(_Float16*)(page + P::kValueScales + 128 * grp + 2 * (32 * half + slot)) = (_Float16)vs;
 #pragma unroll
       for (int i = 0; i < 8; ++i) codes[(d + i) * 32 + slot] = (uint8_t)c[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < D * 4 / 256; ++i) {
+    for (int i = 0; i < kWords; ++i) {
       const int at = tid + 256 * i, d = at >> 2, g = at & 3;
       const u32x2 bytes = *(const u32x2*)(codes + d * 32 + 8 * g);
-      uint32_t w = 0, mask = 0;
+      uint32_t w = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int64_t p = block * 32 + 4 * g + (k & 3) + 16 * (k >> 2);
-        if (p >= first && p < s.end) {
-          w |= (((k < 4 ? bytes.x : bytes.y) >> (8 * (k & 3))) & 15u) << code_bit(k);
-          mask |= 15u << code_bit(k);
-        }
-      }
-      uint32_t* out = (uint32_t*)(page + value_word<D>(half, d, g));
-      if (mask) *out = mask == 0xffffffffu ? w : (w | (*out & ~mask));
+      for (int k = 0; k < 8; ++k) w |= (((k < 4 ? bytes.x : bytes.y) >> (8 * (k & 3))) & 15u) << code_bit(k);
+      if (mask[i]) *(uint32_t*)(page + value_word<D>(half, d, g)) = (w & mask[i]) | (old[i] & ~mask[i]);
     }
     __syncthreads();
   }

@@ -20,8 +20,9 @@ namespace {
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
-constexpr int kHeld = 4;  // runs of 8 elements a thread keeps: 8192 elements a row
+// Up to this many rows a workgroup has 512 threads: half the elements a thread and half the chain
+// (KEEPNOTE).
+constexpr int64_t kFewRows = 256;
 
 struct NormArgs {
   const void* residual;
@@ -109,22 +110,38 @@ __device__ __forceinline__ void scale8(const NormArgs& a, int64_t row, int i, fl
   store8(a.x, row * a.ldx, i, a, a.x_type, h);
 }
 
+// kHeld: the runs of 8 elements that a thread keeps.
+template <int kThreads, int kHeld>
 __global__ __launch_bounds__(kThreads) void vbq_add_norm_kernel(NormArgs a) {
-  __shared__ float part[kThreads / 64];
+  constexpr int kWaves = kThreads / 64, kStep = 8 * kThreads;
+  __shared__ float part[kWaves];
   const int64_t row = blockIdx.x;
   const int first = 8 * (int)threadIdx.x;
-  float h[kHeld][8], total = 0.0f;
+  // (all loads before the first use)
+  float h[kHeld][8], y[kHeld][8], total = 0.0f;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
-    const int i = first + j * 8 * kThreads;
-    if (i >= a.K) break;
-    sum8(a, row, i, h[j]);
-    if (a.h) store8(a.h, row * a.ldh, i, a, a.res_type, h[j]);
+    const int i = first + j * kStep;
+    if (i < a.K) {
+      load8(a.residual, row * a.ldr, i, a, a.res_type, h[j]);
+      if (a.y) load8(a.y, row * a.ldy, i, a, a.y_type, y[j]);
+    }
+  }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) total = __builtin_fmaf(h[j][e], h[j][e], total);
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = first + j * kStep;
+    if (i < a.K) {
+      if (a.y) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[j][e] = rounded(h[j][e] + y[j][e], a.res_type);
+      }
+      if (a.h) store8(a.h, row * a.ldh, i, a, a.res_type, h[j]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) total = __builtin_fmaf(h[j][e], h[j][e], total);
+    }
   }
   // longer rows: the rest is read again for the scaling (from h where it was stored: the residual may be h)
-  for (int i = first + kHeld * 8 * kThreads; i < a.K; i += 8 * kThreads) {
+  for (int i = first + kHeld * kStep; i < a.K; i += kStep) {
     float t[8];
     sum8(a, row, i, t);
     if (a.h) store8(a.h, row * a.ldh, i, a, a.res_type, t);
@@ -135,15 +152,16 @@ __global__ __launch_bounds__(kThreads) void vbq_add_norm_kernel(NormArgs a) {
   for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d, 64);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = total;
   __syncthreads();
-  total = (part[0] + part[1]) + (part[2] + part[3]);
+  total = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kWaves; ++j) total += part[j];
   const float r = 1.0f / __builtin_sqrtf(total / (float)a.K + a.eps);
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
-    const int i = first + j * 8 * kThreads;
-    if (i >= a.K) break;
-    scale8(a, row, i, r, h[j]);
+    const int i = first + j * kStep;
+    if (i < a.K) scale8(a, row, i, r, h[j]);
   }
-  for (int i = first + kHeld * 8 * kThreads; i < a.K; i += 8 * kThreads) {
+  for (int i = first + kHeld * kStep; i < a.K; i += kStep) {
     float t[8];
     if (a.h) load8(a.h, row * a.ldh, i, a, a.res_type, t);
     else sum8(a, row, i, t);
@@ -180,7 +198,11 @@ vbq_status vbq_add_norm(int64_t n_rows, int64_t K, int32_t res_type, const void*
   }
   NormArgs a{residual_dev, y_dev, weight_dev, h_dev, x_dev, ldr, ldy, ldh, ldx, (int32_t)K, res_type, y_type, weight_type, x_type, vec ? 1 : 0, eps};
   void* args[] = {&a};
-  return vbq_detail_hip_status(hipLaunchKernel((const void*)vbq_add_norm_kernel, dim3((unsigned)n_rows), dim3(kThreads), args, 0, (hipStream_t)stream));
+  const int threads = n_rows <= kFewRows ? 512 : 256;
+  const bool shorter = K <= 16 * threads;
+  const void* f = threads == 512 ? (shorter ? (const void*)vbq_add_norm_kernel<512, 2> : (const void*)vbq_add_norm_kernel<512, 4>)
+                                 : (shorter ? (const void*)vbq_add_norm_kernel<256, 2> : (const void*)vbq_add_norm_kernel<256, 4>);
+  return vbq_detail_hip_status(hipLaunchKernel(f, dim3((unsigned)n_rows), dim3((unsigned)threads), args, 0, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -699,7 +699,7 @@ def qat_logit_grad(W, grad, pi, tau, lam, n_bbar=None, dlogits=None, stream=None
 # that the library allocates itself not checked again.)
 if _torch is not None:
     _DTYPES = {_torch.float32: F32, _torch.float16: F16, _torch.bfloat16: BF16}
-    _current_device = _torch.cuda.current_device
+    _current_device = getattr(_torch._C, "_cuda_getDevice", None) or _torch.cuda.current_device
     _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (
         lambda index: _torch.cuda.current_stream(index).cuda_stream)
 
@@ -746,6 +746,8 @@ def _gpu(t, name):
 
 def _rows(t, name, shape, index):
     """A tensor on device `index`, of this shape, whose last dimension is contiguous."""
+    if t.shape == shape and t.is_cuda and t.get_device() == index and t.is_contiguous():
+        return t
     if _gpu(t, name) != index:
         raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
     if t.shape != shape or (t.stride(-1) != 1 and shape[-1] != 1):
