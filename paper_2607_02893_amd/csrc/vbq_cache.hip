@@ -148,8 +148,7 @@ __device__ __forceinline__ float quantize8(const float (&f)[8], int (&code)[8]) 
   const float r = s > 0.0f ? __builtin_amdgcn_rcpf(s) : 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float q = level4(f[i], s, r);
-    code[i] = (q == q ? (int)q : 0) + 8;
+    code[i] = (int)(level4(f[i], s, r) + 8.0f);  // (some code where the scale is NaN)
   }
   return s;
 }
@@ -161,7 +160,8 @@ __device__ __forceinline__ float quantize8(const float (&f)[8], int (&code)[8]) 
 template <int D>
 __global__ __launch_bounds__(256) void vbq_kv_append_kernel(AppendArgs a) {
   using P = PageOf<D>;
-  __shared__ __attribute__((aligned(8))) uint8_t codes[D * 32];  // [element][slot]
+  constexpr int kLine = 36;  // bytes of an element's 32 slots: with 32 eight lanes would write one bank
+  __shared__ __attribute__((aligned(4))) uint8_t codes[D * kLine];  // [element][slot]
   const int tid = (int)threadIdx.x, t = tid >> 3, sub = tid & 7;
   const int h = (int)blockIdx.y, b = (int)blockIdx.z;
   const Seq s = seq_of(a.batch, b);
@@ -218,16 +218,17 @@ __global__ __launch_bounds__(256) void vbq_kv_append_kernel(AppendArgs a) {
       const float vs = quantize8(fv[grp], c);
       if (on && sub == 0) *(_Float16*)(page + P::kValueScales + 128 * grp + 2 * (32 * half + slot)) = (_Float16)vs;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) codes[(d + i) * 32 + slot] = (uint8_t)c[i];
+      for (int i = 0; i < 8; ++i) codes[(d + i) * kLine + slot] = (uint8_t)c[i];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
       const int at = tid + 256 * i, d = at >> 2, g = at & 3;
-      const u32x2 bytes = *(const u32x2*)(codes + d * 32 + 8 * g);
+      const uint32_t* bytes = (const uint32_t*)(codes + d * kLine + 8 * g);
+      const uint32_t lo = bytes[0], hi = bytes[1];
       uint32_t w = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w |= (((k < 4 ? bytes.x : bytes.y) >> (8 * (k & 3))) & 15u) << code_bit(k);
+      for (int k = 0; k < 8; ++k) w |= (((k < 4 ? lo : hi) >> (8 * (k & 3))) & 15u) << code_bit(k);
       if (mask[i]) *(uint32_t*)(page + value_word<D>(half, d, g)) = (w & mask[i]) | (old[i] & ~mask[i]);
     }
     __syncthreads();
