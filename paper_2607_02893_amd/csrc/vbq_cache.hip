@@ -340,6 +340,14 @@ __device__ __forceinline__ f16x8 level_operand(uint32_t w, uint32_t one) {
   return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
+// The larger of two pairs of whole numbers (scales are not negative: their bits order as they do).  The
+// words come as arguments: __builtin_bit_cast of a vector's component takes another component
+// with this compiler.
+__device__ __forceinline__ uint32_t larger16(uint32_t a, uint32_t b) {
+  const u16x2 m = __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b));
+  return __builtin_bit_cast(uint32_t, m);
+}
+
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
@@ -519,10 +527,10 @@ struct Rows {
     }
 
     // ---- the bias moves where a score passes it by 2^8, or a value scale the largest so far
-    u16x2 tops = __builtin_bit_cast(u16x2, k.vs[0][0]);  // (scales are not negative: their bits order as they do)
+    uint32_t top = 0;
 #pragma unroll
-    for (int i = 1; i < 4 * kGroups; ++i) tops = __builtin_elementwise_max(tops, __builtin_bit_cast(u16x2, k.vs[i / 4][i % 4]));
-    const uint32_t top = (uint32_t)(tops.x > tops.y ? tops.x : tops.y) >> 10;
+    for (int i = 0; i < 4 * kGroups; ++i) top = larger16(top, k.vs[i / 4][i % 4]);
+    top = ((top & 0xffffu) > (top >> 16) ? top & 0xffffu : top >> 16) >> 10;
     bool grow = (int)top > e;
     float most[NT];
 #pragma unroll

@@ -465,3 +465,19 @@ def test_nothing_to_do(vbq):
     cache.append(empty, empty, none)
     assert cache.attention(empty, none).shape == (0, 1, 64)
     assert cache.dequant(none)[0].shape == (0, 1, 64)
+
+
+def test_one_large_value_among_small_ones(vbq):
+    """A value scale 2^14 times its neighbours', at every place of a block, equal weights and others."""
+    rng = np.random.default_rng(18)
+    L = 40
+    for factor in (0.0, 1.0):
+        for at in range(L):
+            c = Case(vbq, rng, [L], 1, 64, kv="f32")
+            v = c.v[0].clone()
+            v[at] *= 2.0 ** 14
+            c.cache.append(c.k[0], v, vbq.KVBatch(c.t, c.l, max_rows=L))
+            c.values = [odec.kv_values(_np(v))]
+            q = _rows(rng, 1, 2, 64, "f16") * factor
+            out = c.cache.attention(q, c.batch([1]), out_dtype=torch.float32)
+            _check_attention(out, q, c, [1], 0.125, "f32", what=f"place {at}")
