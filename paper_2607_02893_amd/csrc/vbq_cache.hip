@@ -531,6 +531,15 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < 4 * kGroups; ++i) top = larger16(top, k.vs[i / 4][i % 4]);
     top = ((top & 0xffffu) > (top >> 16) ? top & 0xffffu : top >> 16) >> 10;
+    if (top >= 31) {  // a NaN among them: rows that do not see it keep the others' range
+      top = 0;
+#pragma unroll
+      for (int i = 0; i < 4 * kGroups; ++i) {
+        const uint32_t w = k.vs[i / 4][i % 4], lo = (w >> 10) & 31u, hi = (w >> 26) & 31u;
+        top = lo < 31 && lo > top ? lo : top;
+        top = hi < 31 && hi > top ? hi : top;
+      }
+    }
     bool grow = (int)top > e;
     float most[NT];
 #pragma unroll

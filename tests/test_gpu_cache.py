@@ -481,3 +481,24 @@ def test_one_large_value_among_small_ones(vbq):
             q = _rows(rng, 1, 2, 64, "f16") * factor
             out = c.cache.attention(q, c.batch([1]), out_dtype=torch.float32)
             _check_attention(out, q, c, [1], 0.125, "f32", what=f"place {at}")
+
+
+def test_a_not_finite_position_costs_other_rows_nothing(vbq):
+    """Rows that do not see a NaN value keep their precision, small value scales included."""
+    rng = np.random.default_rng(16)
+    for L, rows, at in ((20, 3, 19), (71, 70, 3), (200, 5, 199)):
+        c = Case(vbq, rng, [L], 1, 128, kv="f32")
+        k, v = c.k[0].clone(), c.v[0] * 1e-3
+        values = odec.kv_values(_np(v))
+        v = v.clone()
+        v[at, 0, 7] = float("nan")
+        c.cache.append(k, v, vbq.KVBatch(c.t, c.l, max_rows=L))
+        q = _rows(rng, rows, 2, 128, "f16")
+        out = c.cache.attention(q, c.batch([rows]), out_dtype=torch.float32)
+        n = at - (L - rows)  # rows that do not see it
+        assert torch.isnan(out[n:, :, :64]).all() and torch.isfinite(out[n:, :, 64:]).all()
+
+        class Before:
+            hkv, d = 1, 128
+        Before.keys, Before.values, Before.lens = [c.keys[0][:at]], [values[:at]], [at]
+        _check_attention(out[:n], q[:n], Before, [n], 128 ** -0.5, "f32", what=f"beside NaN, L={L}")
