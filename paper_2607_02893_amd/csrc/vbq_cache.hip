@@ -643,10 +643,9 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
     const int stop = (int)(split + 1) * (int64_t)per < pages ? (int)(split + 1) * per : pages;
     const int64_t heads = (int64_t)a.heads * a.group;
     if (split && split * (int64_t)per >= pages) {  // nothing to see in this part: the join reads no more of it than that
-      if ((int)threadIdx.x < kRows && tile * kRows + threadIdx.x < n_rows) {
-        const uint32_t i = tile * kRows + threadIdx.x;
+      const uint32_t i = base + lane;  // (each wave for its own rows; where they share them, the first)
+      if (lane < 16 * NT && i < n_rows && (kWaveRows || wave == 0))
         store_bias<D>(a, (s.row0 + i / group) * heads + hq0 + i % group, (int)split, 0.0f, 0.0f);
-      }
       continue;
     }
     // What is no page of the cache is read as page 0 and hidden.  Ids are read a page ahead, the

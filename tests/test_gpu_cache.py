@@ -483,6 +483,19 @@ def test_one_large_value_among_small_ones(vbq):
             _check_attention(out, q, c, [1], 0.125, "f32", what=f"place {at}")
 
 
+@pytest.mark.parametrize("d,L,rows", [(64, 16450, 130), (128, 8300, 150), (256, 8240, 90)])
+def test_parts_that_end_among_a_tiles_rows(vbq, d, L, rows):
+    """Split positions whose last part only the later rows of a tile see: every row has its own parts."""
+    rng = np.random.default_rng(15 + d)
+    _say(f"parts d={d} L={L} rows={rows}")
+    c = Case(vbq, rng, [L], 1, d)
+    b = c.batch([rows])
+    assert c.cache.attention_workspace_size(b, 1) > 0, "this case is meant to split the positions"
+    q = torch.zeros((rows, 1, d), dtype=torch.float16, device="cuda")
+    out = c.cache.attention(q, b, out_dtype=torch.float32)
+    _check_attention(out, q, c, [rows], 0.125, "f32", what=f"parts d={d}")
+
+
 def test_a_not_finite_position_costs_other_rows_nothing(vbq):
     """Rows that do not see a NaN value keep their precision, small value scales included."""
     rng = np.random.default_rng(16)
