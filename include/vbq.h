@@ -489,7 +489,7 @@ vbq_status vbq_qat_logit_grad(int64_t n_groups, const float* W_dev,
  * Between the products of a decode step: the residual sum and norm that make
  * the next x, the cache of keys and values with the attention that reads it,
  * and the choice of a token.  These calls follow the conventions at the top of
- * this header; "type" is one of vbq_dtype.
+ * this header; "type" is one of vbq_dtype, and the current device is the stream's.
  * ------------------------------------------------------------------------- */
 typedef enum vbq_dtype { VBQ_F32 = 0, VBQ_F16 = 1, VBQ_BF16 = 2 } vbq_dtype;
 
@@ -621,8 +621,8 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
  * positions that a row does not see does not matter, NaN included.
  *   q_dev, out_dev   [n_rows][n_q_heads][D] of q_type, out_type, with row and
  *             head strides in elements (multiples of 8; out's >= D), 16-byte
- *             aligned; they may not overlap.  |q| below 2^100.
- *   scale     2^-60 .. 2^60, e.g. 1/sqrt(D).
+ *             aligned; they may not overlap.  |q| below 2^60.
+ *   scale     2^-60 .. 2^30, e.g. 1/sqrt(D).
  *   workspace_dev    16-byte aligned scratch of at least
  *             vbq_kv_attention_workspace_size bytes, not shared by calls that
  *             may overlap (NULL where that is 0).

@@ -438,7 +438,7 @@ struct Rows {
     amax = group_max(amax);
     const int ex = (int)(__float_as_uint(amax) >> 23);
     int up = ex == 0 || ex == 255 ? 0 : 141 - ex;
-    up = up > 120 ? 120 : up;
+    up = up > 80 ? 80 : up;  // (c stays a normal number, so hidden scores stay -inf)
     c[nt] = __builtin_ldexpf(a.scale * kLog2e, 24 - up);
 #pragma unroll
     for (int grp = 0; grp < kGroups; ++grp) {
@@ -970,7 +970,7 @@ vbq_status vbq_kv_attention(const vbq_kv_desc* desc, const void* cache_dev, cons
   if (st != VBQ_OK) return st;
   if (!known(q_type) || !known(out_type)) return VBQ_ERR_UNSUPPORTED;
   if (!(scale == scale) || scale == __builtin_inff() || scale == -__builtin_inff()) return VBQ_ERR_NONFINITE;
-  if (!(scale >= 0x1p-60f && scale <= 0x1p60f)) return VBQ_ERR_UNSUPPORTED;
+  if (!(scale >= 0x1p-60f && scale <= 0x1p30f)) return VBQ_ERR_UNSUPPORTED;
   if (batch->n_seqs == 0 || batch->n_rows == 0) return VBQ_OK;
   if (!cache_dev || !q_dev || !out_dev) return VBQ_ERR_NULL;
   if (!strides_fit(ldq, hsq, 0) || !strides_fit(ldo, hso, desc->head_dim)) return VBQ_ERR_SHAPE;

@@ -146,11 +146,13 @@ def test_cache_call_arguments():
         assert _append(d, b, **kw) == want, kw
     for kw, want in ((dict(heads=3), 2), (dict(heads=0), 2), (dict(heads=2 * 257), 2), (dict(qt=3), 10), (dict(ot=-1), 10),
                      (dict(scale=float("nan")), 5), (dict(scale=float("inf")), 5), (dict(scale=0.0), 10), (dict(scale=-1.0), 10),
-                     (dict(scale=1e30), 10), (dict(cache=None), 1), (dict(q=None), 1), (dict(out=None), 1), (dict(ldq=4), 2),
+                     (dict(scale=1e30), 10), (dict(scale=2.0 ** 31), 10), (dict(scale=2.0 ** -61), 10), (dict(cache=None), 1), (dict(q=None), 1), (dict(out=None), 1), (dict(ldq=4), 2),
                      (dict(ldo=64), 2), (dict(hso=0), 2), (dict(q=A + 8), 7), (dict(out=A + 8), 7), (dict(cache=A + 16), 7)):
         assert _attention(d, b, **kw) == want, kw
     for args, want in (((None, A, A), 1), ((A, None, A), 1), ((A, A, None), 1), ((A + 8, A, A), 7), ((A, A + 4, A), 7), ((A, A, A + 8), 7)):
         assert vbq.lib().vbq_kv_dequant(d, args[0], b, args[1], args[2], None) == want
+    many = ctypes.byref(_batch(row_start=A, n_rows=1 << 29))  # rows times query heads a kv head beyond 2^30
+    assert _attention(d, many, heads=8) == 2
     # a long cache splits the positions: the workspace is asked for and checked
     long = ctypes.byref(_batch(table_stride=4096, max_len=4096 * 64))
     n = ctypes.c_size_t(0)

@@ -515,3 +515,14 @@ def test_a_not_finite_position_costs_other_rows_nothing(vbq):
             hkv, d = 1, 128
         Before.keys, Before.values, Before.lens = [c.keys[0][:at]], [values[:at]], [at]
         _check_attention(out[:n], q[:n], Before, [n], 128 ** -0.5, "f32", what=f"beside NaN, L={L}")
+
+
+def test_scores_at_the_ends_of_their_range(vbq):
+    """Scales and queries at both ends of what is allowed, with hidden positions beside them."""
+    rng = np.random.default_rng(17)
+    c = Case(vbq, rng, [45], 1, 64)
+    q = _rows(rng, 4, 2, 64, "f32")
+    for factor, scale in ((2.0 ** -100, 2.0 ** -60), (2.0 ** -60, 2.0 ** 30), (2.0 ** 30, 2.0 ** -40), (0.0, 2.0 ** -60)):
+        x = q * factor
+        out = c.cache.attention(x, c.batch([4]), scale=scale, out_dtype=torch.float32)
+        _check_attention(out, x, c, [4], scale, "f32", what=f"factor {factor} scale {scale}")
