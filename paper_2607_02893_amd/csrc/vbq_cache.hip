@@ -606,18 +606,19 @@ __device__ __forceinline__ void store_bias(const AttnArgs& a, int64_t row_head, 
   at[1] = sum;
 }
 
-// Row tiles of a wave that has rows of its own: what its registers hold.
-constexpr int wave_tiles(int D) { return D == 256 ? 1 : 2; }
-constexpr int waves_per_simd(int D, int NT) { return D * NT <= 64 ? 4 : D * NT <= 128 ? 3 : 2; }
+constexpr int waves_per_simd(int D, int NT) { return NT > 1 || D > 128 ? 2 : D > 64 ? 3 : 4; }
 
-// kWaveRows: the four waves take different rows and walk the same positions;
-// otherwise they take the same rows and every fourth page each, and join at the end.
-template <int D, int NT, bool kTwoTerms, bool kWaveRows>
+// A workgroup takes a tile of 16 NT rows (query heads of one kv head, row by row) and a part of
+// the positions; its waves take every fourth page each and join at the end, a lane's sums through LDS.
+// Rows of their own for the waves (no join, each page read by all four) came to the same on grids
+// that fill the chip (2 x 2048 rows of 32 heads over 6144 positions 514 us, so 527) and to two to six times
+// as long on smaller ones (256 rows over 16384: 284 us, so 46), where a wave walks all positions.
+template <int D, int NT, bool kTwoTerms>
 __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_attention_kernel(AttnArgs a) {
   using P = PageOf<D>;
-  constexpr int kRows = 16 * NT * (kWaveRows ? kWaves : 1);
-  __shared__ __attribute__((aligned(16))) float o_lds[kWaveRows ? 1 : kWaves][kWaveRows ? 1 : kRows][kWaveRows ? 4 : D + 4];
-  __shared__ float bias_lds[kWaveRows ? 1 : kWaves][kWaveRows ? 1 : kRows], sum_lds[kWaveRows ? 1 : kWaves][kWaveRows ? 1 : kRows];
+  constexpr int kRows = 16 * NT;
+  __shared__ __attribute__((aligned(16))) float o_lds[kWaves][kRows][D + 4];
+  __shared__ float bias_lds[kWaves][kRows], sum_lds[kWaves][kRows];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, g = lane >> 4;
   const uint32_t h = blockIdx.x % (uint32_t)a.heads, split = blockIdx.x / (uint32_t)a.heads, group = (uint32_t)a.group;
   const int b = (int)blockIdx.y;
@@ -627,7 +628,7 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
 
   // the last tiles see the most positions: they start first
   for (uint32_t tile = gridDim.z - 1 - blockIdx.z; tile * kRows < n_rows; tile += gridDim.z) {
-    const uint32_t base = tile * kRows + (kWaveRows ? wave * 16 * NT : 0);
+    const uint32_t base = tile * kRows;
     Rows<D, NT, kTwoTerms> r;
     r.e = 0;
     asm("v_mov_b32 %0, 0x64006400" : "=v"(r.one));
@@ -636,15 +637,15 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
       const int64_t v = s.pos0 + row + 1;
       return (int)(v < 0 ? 0 : v < s.end ? v : s.end);
     };
-    const int least = base < n_rows ? seen(base / group) : 0, most = base < n_rows ? seen((last - 1) / group) : 0;
+    const int least = seen(base / group), most = seen((last - 1) / group);
     const int pages = (most + kPage - 1) / kPage, least_per = (pages + a.splits - 1) / a.splits;
-    const int per = a.split_pages > least_per ? a.split_pages : least_per, step = kWaveRows ? 1 : kWaves;
-    const int64_t first = (int64_t)split * per + (kWaveRows ? 0 : wave);
+    const int per = a.split_pages > least_per ? a.split_pages : least_per;
+    const int64_t first = (int64_t)split * per + wave;
     const int stop = (int)(split + 1) * (int64_t)per < pages ? (int)(split + 1) * per : pages;
     const int64_t heads = (int64_t)a.heads * a.group;
     if (split && split * (int64_t)per >= pages) {  // nothing to see in this part: the join reads no more of it than that
-      const uint32_t i = base + lane;  // (each wave for its own rows; where they share them, the first)
-      if (lane < 16 * NT && i < n_rows && (kWaveRows || wave == 0))
+      const uint32_t i = base + threadIdx.x;
+      if (threadIdx.x < kRows && i < n_rows)
         store_bias<D>(a, (s.row0 + i / group) * heads + hq0 + i % group, (int)split, 0.0f, 0.0f);
       continue;
     }
@@ -656,7 +657,7 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
     };
     Block<D> k;
     int page = (int)(first < stop ? first : stop), half = 0;
-    int64_t id = id_of(first), next = id_of(first + step);
+    int64_t id = id_of(first), next = id_of(first + kWaves);
     if (page < stop) load(k, id, 0);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -669,10 +670,10 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
     while (page < stop) {
       const int pos = id < 0 ? kNowhere : page * kPage + 32 * half;
       if (half || page * kPage + 32 >= most) {  // the next block is another page's first
-        page += step;
+        page += kWaves;
         id = next;
         half = 0;
-        next = id_of((int64_t)page + step);
+        next = id_of((int64_t)page + kWaves);
       } else {
         half = 1;
       }
@@ -680,79 +681,52 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
       if (page < stop) load(k, id, half);
     }
 
-    if constexpr (kWaveRows) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint32_t i = base + 16 * nt + (lane & 15);
-        const float sum = group_sum(r.sum[nt]);
-        if (i >= n_rows) continue;
-        const int64_t row = s.row0 + i / group;
-        const int64_t hq = hq0 + i % group;
-        if (a.splits == 1) {
-          const float f = sum == 0.0f ? 0.0f : 1.0f / sum;  // (the sums of a row that sees nothing are 0)
-          const int64_t at = row * a.ldo + hq * a.hso + 4 * g;
-          if (a.out_type == VBQ_F32) {
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) *(f32x4*)((float*)a.out + at + 16 * d) = r.o[nt][d] * f;
-          } else {
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) store4(a.out, at + 16 * d, a.out_type, r.o[nt][d] * f);
-          }
-        } else {
-          const int64_t rh = row * heads + hq;
-          if (g == 0) store_bias<D>(a, rh, split, r.bias(nt), sum);
-#pragma unroll
-          for (int d = 0; d < D / 16; ++d) *(f32x4*)(a.part + (rh * a.splits + split) * D + 16 * d + 4 * g) = r.o[nt][d];
-        }
+    for (int nt = 0; nt < NT; ++nt) {
+      const float sum = group_sum(r.sum[nt]);
+      const int i = 16 * nt + (lane & 15);
+      if (g == 0) {
+        bias_lds[wave][i] = r.bias(nt);
+        sum_lds[wave][i] = sum;
       }
-    } else {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float sum = group_sum(r.sum[nt]);
-        const int i = 16 * nt + (lane & 15);
-        if (g == 0) {
-          bias_lds[wave][i] = r.bias(nt);
-          sum_lds[wave][i] = sum;
-        }
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) *(f32x4*)&o_lds[wave][i][16 * d + 4 * g] = r.o[nt][d];
-      }
-      __syncthreads();
-      constexpr int kLanes = 256 / kRows, kEach = D / kLanes;  // lanes of a row, elements of a lane
-      const int i = (int)threadIdx.x / kLanes, sub = (int)threadIdx.x % kLanes;
-      const uint32_t ri = base + i;
-      if (ri < n_rows) {
-        float top = -__builtin_inff(), f[kWaves], sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          f[w] = sum_lds[w][i] == 0.0f ? -__builtin_inff() : bias_lds[w][i];
-          top = __builtin_fmaxf(top, f[w]);
-        }
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          // (a wave that saw nothing of the row, or only NaN biases, adds its sum as it is)
-          f[w] = f[w] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(f[w] - top);
-          sum += sum_lds[w][i] * f[w];
-        }
-        const int64_t row = s.row0 + ri / group;
-        const int64_t hq = hq0 + ri % group;
-        const int64_t rh = row * heads + hq;
-        const float scale = a.splits > 1 ? 1.0f : 1.0f / sum;
-        if (a.splits > 1 && sub == 0) store_bias<D>(a, rh, split, top == -__builtin_inff() ? 0.0f : top, sum);
-#pragma unroll
-        for (int d = 0; d < kEach; d += 4) {
-          f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int w = 0; w < kWaves; ++w) {
-            if (f[w] != 0.0f) v += *(const f32x4*)&o_lds[w][i][4 * (sub + kLanes * (d / 4))] * f[w];
-          }
-          const int el = 4 * (sub + kLanes * (d / 4));
-          if (a.splits > 1) *(f32x4*)(a.part + (rh * a.splits + split) * D + el) = v;
-          else store4(a.out, row * a.ldo + hq * a.hso + el, a.out_type, sum == 0.0f ? v : v * scale);
-        }
-      }
-      __syncthreads();
+      for (int d = 0; d < D / 16; ++d) *(f32x4*)&o_lds[wave][i][16 * d + 4 * g] = r.o[nt][d];
     }
+    __syncthreads();
+    constexpr int kLanes = 256 / kRows, kEach = D / kLanes;  // lanes of a row, elements of a lane
+    const int i = (int)threadIdx.x / kLanes, sub = (int)threadIdx.x % kLanes;
+    const uint32_t ri = base + i;
+    if (ri < n_rows) {
+      float top = -__builtin_inff(), f[kWaves], sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        f[w] = sum_lds[w][i] == 0.0f ? -__builtin_inff() : bias_lds[w][i];
+        top = __builtin_fmaxf(top, f[w]);
+      }
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        // (a wave that saw nothing of the row, or only NaN biases, adds its sum as it is)
+        f[w] = f[w] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(f[w] - top);
+        sum += sum_lds[w][i] * f[w];
+      }
+      const int64_t row = s.row0 + ri / group;
+      const int64_t hq = hq0 + ri % group;
+      const int64_t rh = row * heads + hq;
+      const float scale = a.splits > 1 ? 1.0f : 1.0f / sum;
+      if (a.splits > 1 && sub == 0) store_bias<D>(a, rh, split, top == -__builtin_inff() ? 0.0f : top, sum);
+#pragma unroll
+      for (int d = 0; d < kEach; d += 4) {
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          if (f[w] != 0.0f) v += *(const f32x4*)&o_lds[w][i][4 * (sub + kLanes * (d / 4))] * f[w];
+        }
+        const int el = 4 * (sub + kLanes * (d / 4));
+        if (a.splits > 1) *(f32x4*)(a.part + (rh * a.splits + split) * D + el) = v;
+        else store4(a.out, row * a.ldo + hq * a.hso + el, a.out_type, sum == 0.0f ? v : v * scale);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -847,25 +821,30 @@ Batch batch_of(const vbq_kv_batch* b) {
 }
 
 struct Plan {
-  bool wave_rows;
+  int nt;  // 16-row tiles of a workgroup
   int tiles, splits, split_pages;
 };
 
 Plan plan_of(const vbq_kv_desc* d, const vbq_kv_batch* b, int group) {
   Plan p;
   const int64_t rows = (b->max_rows < b->n_rows ? b->max_rows : b->n_rows) * (int64_t)group;
-  p.wave_rows = rows > 64;
-  const int64_t per = p.wave_rows ? 16 * kWaves * wave_tiles(d->head_dim) : 16, tiles = (rows + per - 1) / per;
   const int64_t units = (int64_t)b->n_seqs * d->n_heads, most = kMaxGrid / kMaxSplits / units;  // (the kernel's loop takes the rest)
+  // 32 rows share a page's loads and conversions where workgroups of them are many (us, 16 / 32 rows,
+  // 128 elements, 4096 positions: 128 of them 38.6 / 35.6, 512 138 / 115; 64 16.1 / 28.4); with 256
+  // elements their sums do not fit the registers.
+  p.nt = d->head_dim <= 128 && units * ((rows + 31) / 32) >= 128 ? 2 : 1;
+  const int64_t per = 16 * p.nt, tiles = (rows + per - 1) / per;
   p.tiles = (int)(tiles < 16384 ? tiles : 16384);
   if (p.tiles > most) p.tiles = most > 1 ? (int)most : 1;
   // Parts of equal size whatever a sequence's length, so that long sequences of a ragged batch get
-  // more workgroups: as many as the chip holds at a time if all were max_len long, no part below a page
-  // a wave, nor so small that its sums (4 D bytes a row, written and read) cost a tenth of its pages.
+  // more workgroups: at 64 and 128 elements twice as many as the chip holds at a time if all were
+  // max_len long (once / twice, a ragged batch of eight: 22.7 / 21.6 us), at 256 as many (sixteen
+  // sequences 34.7 / 39.1); no part below a page a wave, nor so small that its sums
+  // (4 D bytes a row, written and read) cost a tenth of its pages.
   const int64_t base = units * p.tiles, pages = ((int64_t)b->max_len + kPage - 1) / kPage;
-  const int64_t want = (p.wave_rows ? 512 : 256 * (d->head_dim == 256 ? 2 : 6)) / base;
+  const int64_t want = (p.nt > 1 || d->head_dim == 256 ? 512 : 1536) / base;
   int64_t part = want > 1 ? (pages + want - 1) / want : pages;
-  const int64_t most_parts = (pages + kMaxSplits - 1) / kMaxSplits, tile_rows = rows < per ? rows : per;
+  const int64_t most_parts = (pages + kMaxSplits - 1) / kMaxSplits, tile_rows = rows < 16 ? rows : 16;
   part = part < kWaves ? kWaves : part;
   part = part < tile_rows ? tile_rows : part;
   part = part < most_parts ? most_parts : part;
@@ -876,9 +855,10 @@ Plan plan_of(const vbq_kv_desc* d, const vbq_kv_batch* b, int group) {
 
 template <int D>
 const void* attention_kernel(const Plan& p, bool two_terms) {
-  constexpr int NT = wave_tiles(D);
-  if (p.wave_rows) return two_terms ? (const void*)vbq_kv_attention_kernel<D, NT, true, true> : (const void*)vbq_kv_attention_kernel<D, NT, false, true>;
-  return two_terms ? (const void*)vbq_kv_attention_kernel<D, 1, true, false> : (const void*)vbq_kv_attention_kernel<D, 1, false, false>;
+  if constexpr (D <= 128) {
+    if (p.nt == 2) return two_terms ? (const void*)vbq_kv_attention_kernel<D, 2, true> : (const void*)vbq_kv_attention_kernel<D, 2, false>;
+  }
+  return two_terms ? (const void*)vbq_kv_attention_kernel<D, 1, true> : (const void*)vbq_kv_attention_kernel<D, 1, false>;
 }
 
 vbq_status launch(const void* f, dim3 grid, int threads, void** args, void* stream) {

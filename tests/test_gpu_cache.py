@@ -262,13 +262,18 @@ SHAPES = [  # d, hkv, group, lens, rows
     (64, 1, 16, [80, 130, 64], [4, 2, 1]),
     (128, 1, 20, [90, 33], [1, 3]),                           # a group that is no divisor of 16
     (256, 2, 2, [40, 129], [9, 1]),
-    (128, 2, 4, [150, 64, 97, 20], [150, 17, 1, 40]),         # enough rows for the waves to take rows
+    (128, 2, 4, [150, 64, 97, 20], [150, 17, 1, 40]),
     (64, 1, 1, [200, 333], [200, 90]),
     (256, 1, 4, [130, 70], [60, 33]),
     (128, 4, 1, [3000, 17, 0, 1111], [1, 1, 0, 1]),           # split positions
     (64, 1, 6, [5001], [3]),
     (256, 1, 2, [2050], [1]),
-    (128, 1, 2, [2500], [70]),                                # split, the waves taking rows
+    (128, 1, 2, [2500], [70]),
+    (64, 8, 4, [100, 90], [64, 50]),                          # many tiles: 32 rows of a workgroup
+    (128, 8, 4, [70, 131], [70, 40]),
+    (64, 8, 4, [4200, 300], [64, 60]),                        # the same, split
+    (128, 16, 2, [1500, 40, 0, 200], [33, 40, 3, 64]),
+    (64, 1, 256, [70], [1]),                                  # the largest group
 ]
 
 
@@ -526,3 +531,17 @@ def test_scores_at_the_ends_of_their_range(vbq):
         x = q * factor
         out = c.cache.attention(x, c.batch([4]), scale=scale, out_dtype=torch.float32)
         _check_attention(out, x, c, [4], scale, "f32", what=f"factor {factor} scale {scale}")
+
+
+def test_calls_on_two_streams_at_once(vbq):
+    rng = np.random.default_rng(19)
+    c = Case(vbq, rng, [3000, 900, 2000], 2, 128)
+    q = [_rows(rng, 3, 8, 128, "f16") for _ in range(2)]
+    b = c.batch([1, 1, 1])
+    want = [c.cache.attention(x, b) for x in q]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[c.cache.attention(q[i], b, stream=streams[i]) for i in range(2)] for _ in range(20)]
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o[0], want[0]) and torch.equal(o[1], want[1])

@@ -204,3 +204,23 @@ def test_streams_and_graphs(vbq):
             graphs[i].replay()
             torch.cuda.synchronize()
             assert torch.equal(toks[i], vbq.sample(zs[i], u, None, k, p)[0]), (step, i)
+
+
+def test_more_rows_than_are_taken_at_once(vbq):
+    """Long rows come in sets that share the workspace, one after the other."""
+    rng = np.random.default_rng(8)
+    z = _dev(3 * rng.standard_normal((150, 4500)))
+    _check(vbq, z, rng.uniform(0, 1, 150), rng.uniform(0.5, 1.4, 150), rng.integers(0, 300, 150), rng.uniform(0.3, 1.1, 150))
+
+
+def test_calls_on_two_streams_at_once(vbq):
+    rng = np.random.default_rng(9)
+    z = [_dev(3 * rng.standard_normal((4, 20000))) for _ in range(2)]
+    u, k, p = _dev(rng.uniform(0, 1, 4)), _dev(np.array([0, 40, 0, 300]), np.int32), _dev(np.array([0.9, 0.8, 1.0, 1.0]))
+    want = [vbq.sample(x, u, None, k, p)[0] for x in z]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[vbq.sample(z[i], u, None, k, p, stream=streams[i])[0] for i in range(2)] for _ in range(20)]
+    torch.cuda.synchronize()
+    for g in got:
+        assert torch.equal(g[0], want[0]) and torch.equal(g[1], want[1])
