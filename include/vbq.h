@@ -557,8 +557,8 @@ typedef struct vbq_kv_desc {
 } vbq_kv_desc;
 
 /* Fills *desc_out for a cache of n_pages pages.  Errors: NULL, SHAPE (n_pages
- * outside [1, 2^31), n_heads outside [1, VBQ_KV_MAX_HEADS]), UNSUPPORTED (head_dim not 64,
- * 128 or 256). */
+ * outside [1, 2^31), n_heads outside [1, VBQ_KV_MAX_HEADS]), UNSUPPORTED
+ * (head_dim not 64, 128 or 256). */
 vbq_status vbq_kv_layout(int64_t n_pages, int32_t n_heads, int32_t head_dim,
                          vbq_kv_desc* desc_out);
 
@@ -566,11 +566,11 @@ vbq_status vbq_kv_layout(int64_t n_pages, int32_t n_heads, int32_t head_dim,
  * out); sequence b owns rows row_start[b] .. row_start[b+1]-1, or max_rows rows
  * each with row_start NULL (n_rows == n_seqs * max_rows then).  seq_len[b]
  * counts its positions, this call's rows included: the last of its n rows is at
- * position seq_len[b] - 1, its row r at seq_len[b] - n + r.  The arrays are device memory, read
- * when the kernel runs.  Whatever they hold, rows outside [0, n_rows),
- * positions below 0 or beyond table_stride pages, and pages outside
- * [0, n_pages) are neither read nor written; what that leaves out is said at
- * each call.  Rows of no sequence are left as they are. */
+ * position seq_len[b] - 1, its row r at seq_len[b] - n + r.  The arrays are
+ * device memory, read when the kernel runs.  Whatever they hold, rows outside
+ * [0, n_rows), positions below 0 or beyond table_stride pages, and pages
+ * outside [0, n_pages) are neither read nor written; what that leaves out is
+ * said at each call.  Rows of no sequence are left as they are. */
 typedef struct vbq_kv_batch {
   int32_t n_seqs;                 /* 0 .. VBQ_KV_MAX_SEQS                      */
   int32_t table_stride;           /* entries of a sequence in page_table       */
@@ -585,12 +585,12 @@ typedef struct vbq_kv_batch {
 
 /* Quantizes the rows of k and v into their positions' places in the cache.
  * k, v: [n_rows][n_heads][D] of one type with row strides ldk, ldv and head
- * strides hsk, hsv in elements (multiples of 8; pointers 16-byte aligned), such as the
- * K and V columns of a fused projection's y.  No two sequences of a call may
- * own the same page where they write, nor may calls that may overlap.  Rows at no position or page are
- * dropped.  cache_dev: desc->total_bytes bytes, 256-byte aligned; its other
- * positions keep their contents.  Errors: NULL, DESC, SHAPE, UNSUPPORTED
- * (type), BUFFER, HIP. */
+ * strides hsk, hsv in elements (multiples of 8; pointers 16-byte aligned), such
+ * as the K and V columns of a fused projection's y.  No two sequences of a call
+ * may own the same page where they write, nor may calls that may overlap.  Rows
+ * at no position or page are dropped.  cache_dev: desc->total_bytes bytes,
+ * 256-byte aligned; its other positions keep their contents.  Errors: NULL,
+ * DESC, SHAPE, UNSUPPORTED (type), BUFFER, HIP. */
 vbq_status vbq_kv_append(const vbq_kv_desc* desc, void* cache_dev,
                          const vbq_kv_batch* batch, int32_t type,
                          const void* k_dev, int64_t ldk, int64_t hsk,
@@ -614,11 +614,11 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
 
 /* Attention of the call's query rows over the cache:
  *   out[r][i] = sum_p softmax_p(scale * q[r][i] . k_p) v_p
- * with k_p, v_p of kv head i / (n_q_heads / n_heads) as vbq_kv_dequant gives them,
- * over the positions p from 0 up to the row's own (so its own key and value are to be
- * appended first).  A row that sees no position (before position 0, or all its
- * pages outside the cache) gives zeros; what the cache holds at
- * positions that a row does not see does not matter, NaN included.
+ * with k_p, v_p of kv head i / (n_q_heads / n_heads) as vbq_kv_dequant gives
+ * them, over the positions p from 0 up to the row's own (so its own key and
+ * value are to be appended first).  A row that sees no position (before
+ * position 0, or all its pages outside the cache) gives zeros; what the cache
+ * holds at positions that a row does not see does not matter, NaN included.
  *   q_dev, out_dev   [n_rows][n_q_heads][D] of q_type, out_type, with row and
  *             head strides in elements (multiples of 8; out's >= D), 16-byte
  *             aligned; they may not overlap.  |q| below 2^60.
@@ -629,9 +629,9 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
  * Sums and softmax statistics are fp32; a position's weight times its value
  * scale is rounded to fp16 (2^-11 of the term), fp32 queries are taken as two
  * fp16 terms, others as they are.  Sums are taken in a fixed order.
- * Errors: NULL, DESC, SHAPE (n_q_heads not a multiple of n_heads, more
- * than VBQ_KV_MAX_GROUP each, n_rows times their number a kv head above 2^30, strides), UNSUPPORTED (types, scale), NONFINITE
- * (scale), BUFFER, HIP. */
+ * Errors: NULL, DESC, SHAPE (n_q_heads not a multiple of n_heads, more than
+ * VBQ_KV_MAX_GROUP query heads a kv head, n_rows times that number above 2^30,
+ * strides), UNSUPPORTED (types, scale), NONFINITE (scale), BUFFER, HIP. */
 vbq_status vbq_kv_attention(const vbq_kv_desc* desc, const void* cache_dev,
                             const vbq_kv_batch* batch, int32_t n_q_heads,
                             float scale, int32_t q_type, const void* q_dev,

@@ -332,7 +332,8 @@ __device__ __forceinline__ f16x8 code_operand(uint32_t w) {
 // operation then (of two constants it takes only one from elsewhere).
 __device__ __forceinline__ f16x8 level_operand(uint32_t w, uint32_t one) {
   const uint32_t w8 = w >> 8;
-  const f16x2 unit = {(_Float16)-1032.0f, (_Float16)-1032.0f}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, minus = {(_Float16)-72.0f, (_Float16)-72.0f};
+  const f16x2 unit = {(_Float16)-1032.0f, (_Float16)-1032.0f}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+  const f16x2 minus = {(_Float16)-72.0f, (_Float16)-72.0f};
   const f16x2 a = __builtin_bit_cast(f16x2, (w & 0x000f000fu) | one) + unit;
   const f16x2 b = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (w & 0x00f000f0u) | one), sixteenth, minus);
   const f16x2 c = __builtin_bit_cast(f16x2, (w8 & 0x000f000fu) | one) + unit;
@@ -510,7 +511,8 @@ struct Rows {
         for (int nt = 0; nt < NT; ++nt) {
           float s = 0.0f;
 #pragma unroll
-          for (int grp = 0; grp < kGroups; ++grp) s = __builtin_fmaf((float)__builtin_bit_cast(f16x8, k.ks[grp])[4 * t + i], acc[nt][grp][i], s);
+          for (int grp = 0; grp < kGroups; ++grp)
+            s = __builtin_fmaf((float)__builtin_bit_cast(f16x8, k.ks[grp])[4 * t + i], acc[nt][grp][i], s);
           x[nt][4 * t + i] = s;
         }
       }
@@ -544,7 +546,8 @@ struct Rows {
     float most[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      most[nt] = max3(max3(max3(x[nt][0], x[nt][1], x[nt][2]), x[nt][3], x[nt][4]), max3(x[nt][5], x[nt][6], x[nt][7]), x[nt][7]) * c[nt];
+      const float low = max3(max3(x[nt][0], x[nt][1], x[nt][2]), x[nt][3], x[nt][4]);
+      most[nt] = max3(low, max3(x[nt][5], x[nt][6], x[nt][7]), x[nt][7]) * c[nt];
       grow |= most[nt] > mu[nt] + 8.0f;
     }
     if (__builtin_amdgcn_ballot_w64(grow)) {
@@ -779,7 +782,8 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
       v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < kSide; ++j) v += *(const f32x4*)&o_lds[j][el];
-      store4(a.out, (s.row0 + i) * a.ldo + hq * a.hso + el, a.out_type, sum == 0.0f ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : v * (1.0f / sum));
+      const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+      store4(a.out, (s.row0 + i) * a.ldo + hq * a.hso + el, a.out_type, sum == 0.0f ? none : v * (1.0f / sum));
     }
     __syncthreads();
   }
@@ -802,8 +806,10 @@ vbq_status check_desc(const vbq_kv_desc* d) {
 
 vbq_status check_batch(const vbq_kv_batch* b) {
   if (!b) return VBQ_ERR_NULL;
-  if (b->n_seqs < 0 || b->n_seqs > VBQ_KV_MAX_SEQS || b->n_rows < 0 || b->n_rows > VBQ_KV_MAX_ROWS) return VBQ_ERR_SHAPE;
-  if (b->max_rows < 1 || b->max_len < 0 || b->table_stride < 1 || b->table_stride > VBQ_KV_MAX_TABLE) return VBQ_ERR_SHAPE;
+  if (b->n_seqs < 0 || b->n_seqs > VBQ_KV_MAX_SEQS || b->n_rows < 0 || b->n_rows > VBQ_KV_MAX_ROWS)
+    return VBQ_ERR_SHAPE;
+  if (b->max_rows < 1 || b->max_len < 0 || b->table_stride < 1 || b->table_stride > VBQ_KV_MAX_TABLE)
+    return VBQ_ERR_SHAPE;
   if (!b->row_start && b->n_rows != (int64_t)b->n_seqs * b->max_rows) return VBQ_ERR_SHAPE;
   if (b->n_seqs == 0 || b->n_rows == 0) return VBQ_OK;
   if (!b->page_table || !b->seq_len) return VBQ_ERR_NULL;
@@ -856,9 +862,12 @@ Plan plan_of(const vbq_kv_desc* d, const vbq_kv_batch* b, int group) {
 template <int D>
 const void* attention_kernel(const Plan& p, bool two_terms) {
   if constexpr (D <= 128) {
-    if (p.nt == 2) return two_terms ? (const void*)vbq_kv_attention_kernel<D, 2, true> : (const void*)vbq_kv_attention_kernel<D, 2, false>;
+    if (p.nt == 2)
+      return two_terms ? (const void*)vbq_kv_attention_kernel<D, 2, true>
+                       : (const void*)vbq_kv_attention_kernel<D, 2, false>;
   }
-  return two_terms ? (const void*)vbq_kv_attention_kernel<D, 1, true> : (const void*)vbq_kv_attention_kernel<D, 1, false>;
+  return two_terms ? (const void*)vbq_kv_attention_kernel<D, 1, true>
+                   : (const void*)vbq_kv_attention_kernel<D, 1, false>;
 }
 
 vbq_status launch(const void* f, dim3 grid, int threads, void** args, void* stream) {
@@ -932,12 +941,14 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc, const vbq_kv
   vbq_status st = check_desc(desc);
   if (st != VBQ_OK) return st;
   if ((st = check_batch(batch)) != VBQ_OK) return st;
-  if (n_q_heads < 1 || n_q_heads % desc->n_heads || n_q_heads / desc->n_heads > VBQ_KV_MAX_GROUP) return VBQ_ERR_SHAPE;
+  if (n_q_heads < 1 || n_q_heads % desc->n_heads || n_q_heads / desc->n_heads > VBQ_KV_MAX_GROUP)
+    return VBQ_ERR_SHAPE;
   if (batch->n_rows * (n_q_heads / desc->n_heads) > (int64_t)1 << 30) return VBQ_ERR_SHAPE;
   *bytes = 0;
   if (batch->n_seqs == 0 || batch->n_rows == 0) return VBQ_OK;
   const Plan p = plan_of(desc, batch, n_q_heads / desc->n_heads);
-  if (p.splits > 1) *bytes = (size_t)batch->n_rows * (size_t)n_q_heads * (size_t)p.splits * (size_t)(desc->head_dim + 2) * sizeof(float);
+  const size_t row = (size_t)(desc->head_dim + 2) * sizeof(float);
+  if (p.splits > 1) *bytes = (size_t)batch->n_rows * (size_t)n_q_heads * (size_t)p.splits * row;
   return VBQ_OK;
 }
 
@@ -973,7 +984,8 @@ vbq_status vbq_kv_attention(const vbq_kv_desc* desc, const void* cache_dev, cons
                   : D == 128 ? (const void*)vbq_kv_join_kernel<128>
                              : (const void*)vbq_kv_join_kernel<256>;
   const int64_t rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
-  return launch(j, dim3((unsigned)n_q_heads, (unsigned)batch->n_seqs, (unsigned)(rows < 1024 ? rows : 1024)), kWaves * 64, args, stream);
+  const dim3 joins((unsigned)n_q_heads, (unsigned)batch->n_seqs, (unsigned)(rows < 1024 ? rows : 1024));
+  return launch(j, joins, kWaves * 64, args, stream);
 }
 
 }  // extern "C"

@@ -65,7 +65,8 @@ __device__ __forceinline__ void load8(const void* base, int64_t row, int i, cons
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       f[e] = 0.0f;
-      if (i + e < a.K) f[e] = type == VBQ_F32 ? ((const float*)base)[row + i + e] : half_bits(((const uint16_t*)base)[row + i + e], type);
+      if (i + e < a.K)
+        f[e] = type == VBQ_F32 ? ((const float*)base)[row + i + e] : half_bits(((const uint16_t*)base)[row + i + e], type);
     }
   }
 }
@@ -181,7 +182,8 @@ vbq_status vbq_add_norm(int64_t n_rows, int64_t K, int32_t res_type, const void*
                         int64_t ldh, int32_t x_type, void* x_dev, int64_t ldx, void* stream) {
   const int64_t most = (int64_t)1 << 40;
   if (n_rows < 0 || n_rows > INT32_MAX || K < 1 || K > VBQ_NORM_MAX_K) return VBQ_ERR_SHAPE;
-  if (!known(res_type) || !known(x_type) || (y_dev && !known(y_type)) || (weight_dev && !known(weight_type))) return VBQ_ERR_UNSUPPORTED;
+  if (!known(res_type) || !known(x_type) || (y_dev && !known(y_type)) || (weight_dev && !known(weight_type)))
+    return VBQ_ERR_UNSUPPORTED;
   if (!(eps == eps) || eps == __builtin_inff() || eps == -__builtin_inff()) return VBQ_ERR_NONFINITE;
   if (eps < 0.0f) return VBQ_ERR_UNSUPPORTED;
   if (n_rows == 0) return VBQ_OK;
@@ -189,14 +191,16 @@ vbq_status vbq_add_norm(int64_t n_rows, int64_t K, int32_t res_type, const void*
   if (ldr < K || ldx < K || ldr > most || ldx > most || (y_dev && (ldy < K || ldy > most)) || (h_dev && (ldh < K || ldh > most)))
     return VBQ_ERR_SHAPE;
   struct Row { const void* p; int64_t ld; int32_t type; };
-  const Row rows[] = {{residual_dev, ldr, res_type}, {x_dev, ldx, x_type}, {y_dev, ldy, y_type}, {h_dev, ldh, res_type}, {weight_dev, 0, weight_type}};
+  const Row rows[] = {{residual_dev, ldr, res_type}, {x_dev, ldx, x_type}, {y_dev, ldy, y_type}, {h_dev, ldh, res_type},
+                      {weight_dev, 0, weight_type}};
   bool vec = K % 8 == 0;
   for (const Row& r : rows) {
     if (!r.p) continue;
     if ((uintptr_t)r.p % size_of(r.type)) return VBQ_ERR_BUFFER;
     vec = vec && (uintptr_t)r.p % 16 == 0 && r.ld % 8 == 0;
   }
-  NormArgs a{residual_dev, y_dev, weight_dev, h_dev, x_dev, ldr, ldy, ldh, ldx, (int32_t)K, res_type, y_type, weight_type, x_type, vec ? 1 : 0, eps};
+  NormArgs a{residual_dev, y_dev, weight_dev, h_dev, x_dev, ldr, ldy, ldh, ldx, (int32_t)K, res_type, y_type,
+             weight_type, x_type, vec ? 1 : 0, eps};
   void* args[] = {&a};
   const int threads = n_rows <= kFewRows ? 512 : 256;
   const bool shorter = K <= 16 * threads;

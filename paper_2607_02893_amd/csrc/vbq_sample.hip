@@ -647,7 +647,8 @@ __global__ __launch_bounds__(kThreads) void vbq_sample_token_kernel(LongArgs a) 
   if (l.k || l.p < 1.0f) c = find_cuts(bl, st, l, &cuts);
   const uint32_t listed = st.listed;
   if (listed > (uint32_t)kCap) {
-    choose(a.s, bl, row, a.s.V, [&](int i) { return key_at(a.s, row, i); }, [&](int i) { return w.whole(key_at(a.s, row, i)); }, w, l);
+    auto key = [&](int i) { return key_at(a.s, row, i); };
+    choose(a.s, bl, row, a.s.V, key, [&](int i) { return w.whole(key(i)); }, w, l);
     return;
   }
   const int n = (int)listed;
@@ -658,7 +659,8 @@ __global__ __launch_bounds__(kThreads) void vbq_sample_token_kernel(LongArgs a) 
     index[i] = (uint32_t)v;
     bins[i] = (uint16_t)w.bin(keys[i]);
     whole[i] = w.whole(keys[i]);
-    if (i < kRanked) entries[i] = u32x4{keys[i], ((uint32_t)bins[i] << 20) | index[i], (uint32_t)whole[i], (uint32_t)(whole[i] >> 32)};
+    if (i < kRanked)
+      entries[i] = u32x4{keys[i], ((uint32_t)bins[i] << 20) | index[i], (uint32_t)whole[i], (uint32_t)(whole[i] >> 32)};
   }
   if (tid < kMaxChunks) chunk_w[tid] = tid < a.chunks ? st.sum[tid] : 0;
   __syncthreads();
@@ -823,7 +825,8 @@ vbq_status vbq_sample(int64_t M, int64_t V, int32_t type, const void* logits_dev
   SampleArgs a{logits_dev, ld, (int32_t)V, type, temperature_dev, top_k_dev, top_p_dev, min_p_dev, u_dev, token_dev, prob_dev};
   if (V <= kCap) {
     void* args[] = {&a};
-    return vbq_detail_hip_status(hipLaunchKernel((const void*)vbq_sample_row_kernel, dim3((unsigned)M), dim3(kThreads), args, 0, (hipStream_t)stream));
+    return vbq_detail_hip_status(hipLaunchKernel((const void*)vbq_sample_row_kernel, dim3((unsigned)M), dim3(kThreads),
+                                                 args, 0, (hipStream_t)stream));
   }
   LongArgs b{a, (RowState*)workspace_dev, 0, 0, 0};
   split_row(M, V, &b.chunks, &b.per);
@@ -834,7 +837,8 @@ vbq_status vbq_sample(int64_t M, int64_t V, int32_t type, const void* logits_dev
     const int64_t rows = M - b.row0 < kRowsAtOnce ? M - b.row0 : kRowsAtOnce;
     for (const void* f : steps) {
       if (!f) continue;
-      const vbq_status e = vbq_detail_hip_status(hipLaunchKernel(f, dim3((unsigned)(f == steps[3] ? rows : rows * b.chunks)), dim3(kThreads), args, 0, (hipStream_t)stream));
+      const dim3 grid((unsigned)(f == steps[3] ? rows : rows * b.chunks));
+      const vbq_status e = vbq_detail_hip_status(hipLaunchKernel(f, grid, dim3(kThreads), args, 0, (hipStream_t)stream));
       if (e != VBQ_OK) return e;
     }
   }

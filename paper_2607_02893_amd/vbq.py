@@ -828,8 +828,8 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
             h = residual if y is None else _torch.empty(shape, dtype=residual.dtype, device=residual.device)
         if h is not False and (h is not residual or y is not None):
             h_ptr, h_row = h.data_ptr(), row(h, "h")
-        return _lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), row(residual, "residual"), y_type, y_ptr, y_row, w_type, w_ptr, eps,
-                                 h_ptr, h_row, _dtype_of(x, "x"), x.data_ptr(), row(x, "x"), s)
+        return _lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), row(residual, "residual"), y_type, y_ptr, y_row,
+                                 w_type, w_ptr, eps, h_ptr, h_row, _dtype_of(x, "x"), x.data_ptr(), row(x, "x"), s)
 
     _check(_launch(index, stream, call), "vbq_add_norm")
     return x, (None if h is False else h)
@@ -916,8 +916,8 @@ class KVCache:
         if k.dtype != v.dtype:
             raise ValueError("k and v must be of one type")
         data, t = self.data.data_ptr(), _dtype_of(k, "k")
-        _check(_launch(self.index, stream, lambda s: _lib.vbq_kv_append(self._ref, data, ref, t, k_ptr, ldk, hsk, v_ptr, ldv, hsv, s)),
-               "vbq_kv_append")
+        _check(_launch(self.index, stream, lambda s: _lib.vbq_kv_append(self._ref, data, ref, t, k_ptr, ldk, hsk,
+                                                                        v_ptr, ldv, hsv, s)), "vbq_kv_append")
 
     def dequant(self, batch, k=None, v=None, stream=None):
         """(k, v), float32 [n_rows, n_heads, head_dim]: the values the cache holds at the
@@ -997,7 +997,8 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
            stream=None):
     """One token a row (vbq_sample): logits [M, V] (rows may be padded), u float32 [M] the
     random numbers in [0, 1), temperature / top_p / min_p float32 [M] and top_k int32 [M] device tensors or None.
-    probs: a tensor to write into, None to allocate, False to leave out.  Returns (tokens int32 [M], probs float32 [M] or None)."""
+    probs: a tensor to write into, None to allocate, False to leave out.  Returns (tokens int32 [M],
+    probs float32 [M] or None)."""
     index = _gpu(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be [M, V]")
@@ -1028,8 +1029,9 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
         if need and not given:
             scratch = _torch.empty(need, dtype=_torch.uint8, device=dev)
             ws, n = scratch.data_ptr(), need
-        return _lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V, t_ptr, k_ptr,
-                               p_ptr, m_ptr, u_ptr, tokens.data_ptr(), None if probs is False else probs.data_ptr(), ws or None, n, s)
+        return _lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V,
+                               t_ptr, k_ptr, p_ptr, m_ptr, u_ptr, tokens.data_ptr(),
+                               None if probs is False else probs.data_ptr(), ws or None, n, s)
 
     _check(_launch(index, stream, call), "vbq_sample")
     return tokens, (None if probs is False else probs)

@@ -545,3 +545,18 @@ def test_calls_on_two_streams_at_once(vbq):
     torch.cuda.synchronize()
     for o in outs:
         assert torch.equal(o[0], want[0]) and torch.equal(o[1], want[1])
+
+
+def test_not_finite_queries_stay_in_their_rows(vbq):
+    rng = np.random.default_rng(20)
+    c = Case(vbq, rng, [90], 1, 128)
+    for qt in ("f16", "f32", "bf16"):
+        q = _rows(rng, 40, 2, 128, qt)
+        want = c.cache.attention(q, c.batch([40]), out_dtype=torch.float32)
+        for bad in (float("nan"), float("inf")):
+            x = q.clone()
+            x[7, 1, 100] = bad
+            out = c.cache.attention(x, c.batch([40]), out_dtype=torch.float32)
+            assert torch.isnan(out[7, 1]).all()
+            out[7, 1], want[7, 1] = 0.0, 0.0
+            assert torch.equal(out, want), "rows beside it"
