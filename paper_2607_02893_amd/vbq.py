@@ -704,30 +704,15 @@ if _torch is not None:
         lambda index: _torch.cuda.current_stream(index).cuda_stream)
 
 
-class _OtherStream:
-    """A call on another stream or device than the current one: tensors allocated inside belong to
-    that stream, so a freed scratch tensor is not handed out while the call runs."""
-
-    def __init__(self, index, stream):
-        if stream is not None and stream.device.index != index:
-            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{index}")
-        self._index = index
-        self._context = _torch.cuda.device(index) if stream is None else _torch.cuda.stream(stream)
-
-    def __enter__(self):
-        self._context.__enter__()
-        return _raw_stream(self._index)
-
-    def __exit__(self, *exc):
-        self._context.__exit__(*exc)
-
-
-def _launch(index, stream, call):
-    """call(raw stream) on `stream`, or on the current stream of device `index`."""
-    if stream is None and _current_device() == index:
-        return call(_raw_stream(index))
-    with _OtherStream(index, stream) as s:
-        return call(s)
+def _elsewhere(index, stream):
+    """None where a call on device `index` belongs on the current stream, else the context to make it in:
+    tensors allocated inside belong to that stream, so a freed scratch tensor is not
+    handed out while the call runs."""
+    if stream is None:
+        return None if _current_device() == index else _torch.cuda.device(index)
+    if stream.device.index != index:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{index}")
+    return _torch.cuda.stream(stream)
 
 
 def _dtype_of(t, name):
@@ -791,6 +776,10 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
     itself for in place); None allocates it, False leaves it out.  x is x_dtype (float16, the products' input).
     Returns (x, h), h None where left out (and residual itself where y is None and no h is given)."""
     index = _gpu(residual, "residual")
+    other = _elsewhere(index, stream)
+    if other is not None:
+        with other:
+            return add_norm(residual, y, weight, eps, x, h, x_dtype)
     shape = residual.shape
     if not shape or not shape[-1]:
         raise ValueError("residual must be [..., K] with K >= 1")
@@ -811,27 +800,26 @@ def add_norm(residual, y=None, weight=None, eps=1e-5, x=None, h=None, x_dtype=No
         y_type, y_row, y_ptr = _dtype_of(_rows(y, "y", shape, index), "y"), row(y, "y"), y.data_ptr()
     if weight is not None:
         w_type, w_ptr = _dtype_of(_rows(weight, "weight", (K,), index), "weight"), weight.data_ptr()
-    if x is not None:
-        _spread(_rows(x, "x", shape, index), "x")
+    if x is None:
+        x_row, x = K, _torch.empty(shape, dtype=x_dtype or _torch.float16, device=residual.device)
+    else:
+        x_row = row(_spread(_rows(x, "x", shape, index), "x"), "x")
         if x_dtype is not None and x.dtype != x_dtype:
             raise ValueError(f"x must be {x_dtype}")
-    if h is not None and h is not False:
+    if h is None:
+        if y is None:
+            h = residual  # (already there)
+        else:
+            h = _torch.empty(shape, dtype=residual.dtype, device=residual.device)
+            h_ptr, h_row = h.data_ptr(), K
+    elif h is not False:
         _spread(_rows(h, "h", shape, index), "h")
         if h.dtype != residual.dtype:
             raise ValueError("h must have residual's type")
-
-    def call(s):
-        nonlocal x, h, h_ptr, h_row
-        if x is None:
-            x = _torch.empty(shape, dtype=x_dtype or _torch.float16, device=residual.device)
-        if h is None:
-            h = residual if y is None else _torch.empty(shape, dtype=residual.dtype, device=residual.device)
-        if h is not False and (h is not residual or y is not None):
+        if h is not residual or y is not None:
             h_ptr, h_row = h.data_ptr(), row(h, "h")
-        return _lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), row(residual, "residual"), y_type, y_ptr, y_row,
-                                 w_type, w_ptr, eps, h_ptr, h_row, _dtype_of(x, "x"), x.data_ptr(), row(x, "x"), s)
-
-    _check(_launch(index, stream, call), "vbq_add_norm")
+    _check(_lib.vbq_add_norm(n, K, r_type, residual.data_ptr(), row(residual, "residual"), y_type, y_ptr, y_row, w_type, w_ptr,
+                             eps, h_ptr, h_row, _dtype_of(x, "x"), x.data_ptr(), x_row, _raw_stream(index)), "vbq_add_norm")
     return x, (None if h is False else h)
 
 
@@ -909,34 +897,37 @@ class KVCache:
     def append(self, k, v, batch, stream=None):
         """Quantizes rows k, v [n_rows, n_heads, head_dim] (one type; views such as the columns of a fused
         projection's y will do: strides multiples of 8, 16-byte aligned) into the cache (vbq_kv_append)."""
+        other = _elsewhere(self.index, stream)
+        if other is not None:
+            with other:
+                return self.append(k, v, batch)
         ref = self._batch(batch)
         _gpu(k, "k"), _gpu(v, "v")
         k_ptr, ldk, hsk = self._of_rows(k, "k", batch, self.n_heads)
         v_ptr, ldv, hsv = self._of_rows(v, "v", batch, self.n_heads)
         if k.dtype != v.dtype:
             raise ValueError("k and v must be of one type")
-        data, t = self.data.data_ptr(), _dtype_of(k, "k")
-        _check(_launch(self.index, stream, lambda s: _lib.vbq_kv_append(self._ref, data, ref, t, k_ptr, ldk, hsk,
-                                                                        v_ptr, ldv, hsv, s)), "vbq_kv_append")
+        _check(_lib.vbq_kv_append(self._ref, self.data.data_ptr(), ref, _dtype_of(k, "k"), k_ptr, ldk, hsk, v_ptr, ldv, hsv,
+                                  _raw_stream(self.index)), "vbq_kv_append")
 
     def dequant(self, batch, k=None, v=None, stream=None):
         """(k, v), float32 [n_rows, n_heads, head_dim]: the values the cache holds at the
         positions of the call's rows (vbq_kv_dequant); rows without a place are left as they are
         (uninitialised where allocated here)."""
-        ref, shape = self._batch(batch), (batch.n_rows, self.n_heads, self.head_dim)
+        other = _elsewhere(self.index, stream)
+        if other is not None:
+            with other:
+                return self.dequant(batch, k, v)
+        ref, shape, dev = self._batch(batch), (batch.n_rows, self.n_heads, self.head_dim), self.data.device
         for t, name in ((k, "k"), (v, "v")):
             if t is not None and (_rows(t, name, shape, self.index).dtype != _torch.float32 or not t.is_contiguous()):
                 raise ValueError(f"{name} must be contiguous float32")
-
-        def call(s):
-            nonlocal k, v
-            if k is None:
-                k = _torch.empty(shape, dtype=_torch.float32, device=self.data.device)
-            if v is None:
-                v = _torch.empty(shape, dtype=_torch.float32, device=self.data.device)
-            return _lib.vbq_kv_dequant(self._ref, self.data.data_ptr(), ref, k.data_ptr(), v.data_ptr(), s)
-
-        _check(_launch(self.index, stream, call), "vbq_kv_dequant")
+        if k is None:
+            k = _torch.empty(shape, dtype=_torch.float32, device=dev)
+        if v is None:
+            v = _torch.empty(shape, dtype=_torch.float32, device=dev)
+        _check(_lib.vbq_kv_dequant(self._ref, self.data.data_ptr(), ref, k.data_ptr(), v.data_ptr(), _raw_stream(self.index)),
+               "vbq_kv_dequant")
         return k, v
 
     def attention_workspace_size(self, batch, n_q_heads):
@@ -953,35 +944,33 @@ class KVCache:
         sees its sequence's positions up to its own.  scale: 1/sqrt(head_dim) by default.  out: q's type, or
         out_dtype; rows of no sequence are left as they are (uninitialised where out is allocated here).
         workspace: uint8 tensor of attention_workspace_size bytes, allocated where not given."""
+        other = _elsewhere(self.index, stream)
+        if other is not None:
+            with other:
+                return self.attention(q, batch, scale, out, out_dtype, workspace)
         ref = self._batch(batch)
         _gpu(q, "q")
         if q.dim() != 3:
             raise ValueError("q must be [n_rows, n_q_heads, head_dim]")
         heads = q.shape[1]
         q_ptr, ldq, hsq = self._of_rows(q, "q", batch, heads)
-        q_type = _dtype_of(q, "q")
-        if out is not None:
+        if out is None:
+            out = _torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+        else:
             _gpu(out, "out")
             if out_dtype is not None and out.dtype != out_dtype:
                 raise ValueError(f"out must be {out_dtype}")
             _spread(out, "out")
-        need = self.attention_workspace_size(batch, heads)
-        given = None if workspace is None else (_scratch(workspace, self.index), workspace.numel())
-
-        def call(s):
-            nonlocal out
-            if out is None:
-                out = _torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
-            o_ptr, ldo, hso = self._of_rows(out, "out", batch, heads)
-            ws, n = given or (0, 0)
-            if need and not given:
-                scratch = _torch.empty(need, dtype=_torch.uint8, device=q.device)
-                ws, n = scratch.data_ptr(), need
-            return _lib.vbq_kv_attention(self._ref, self.data.data_ptr(), ref, heads,
-                                         self.head_dim ** -0.5 if scale is None else scale, q_type, q_ptr, ldq, hsq,
-                                         _dtype_of(out, "out"), o_ptr, ldo, hso, ws or None, n, s)
-
-        _check(_launch(self.index, stream, call), "vbq_kv_attention")
+        o_ptr, ldo, hso = self._of_rows(out, "out", batch, heads)
+        ws, n = None, self.attention_workspace_size(batch, heads)
+        if workspace is not None:
+            ws, n = _scratch(workspace, self.index), workspace.numel()
+        elif n:
+            scratch = _torch.empty(n, dtype=_torch.uint8, device=q.device)
+            ws = scratch.data_ptr()
+        _check(_lib.vbq_kv_attention(self._ref, self.data.data_ptr(), ref, heads,
+                                     self.head_dim ** -0.5 if scale is None else scale, _dtype_of(q, "q"), q_ptr, ldq, hsq,
+                                     _dtype_of(out, "out"), o_ptr, ldo, hso, ws, n, _raw_stream(self.index)), "vbq_kv_attention")
         return out
 
 
@@ -1000,10 +989,14 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
     probs: a tensor to write into, None to allocate, False to leave out.  Returns (tokens int32 [M],
     probs float32 [M] or None)."""
     index = _gpu(logits, "logits")
+    other = _elsewhere(index, stream)
+    if other is not None:
+        with other:
+            return sample(logits, u, temperature, top_k, top_p, min_p, tokens, probs, workspace)
     if logits.dim() != 2:
         raise ValueError("logits must be [M, V]")
     M, V = logits.shape
-    f32, i32 = _torch.float32, _torch.int32
+    f32, i32, dev = _torch.float32, _torch.int32, logits.device
     if logits.stride(1) != 1 and V > 1:
         raise ValueError("logits must have unit stride in the last dimension")
     u_ptr = _vector(u, "u", f32, M, index)
@@ -1011,29 +1004,20 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
     k_ptr = None if top_k is None else _vector(top_k, "top_k", i32, M, index)
     p_ptr = None if top_p is None else _vector(top_p, "top_p", f32, M, index)
     m_ptr = None if min_p is None else _vector(min_p, "min_p", f32, M, index)
-    if tokens is not None:
-        _vector(tokens, "tokens", i32, M, index)
-    if probs is not None and probs is not False:
-        _vector(probs, "probs", f32, M, index)
-    need = sample_workspace_size(M, V)
-    given = None if workspace is None else (_scratch(workspace, index), workspace.numel())
-
-    def call(s):
-        nonlocal tokens, probs
-        dev = logits.device
-        if tokens is None:
-            tokens = _torch.empty(M, dtype=i32, device=dev)
-        if probs is None:
-            probs = _torch.empty(M, dtype=f32, device=dev)
-        ws, n = given or (0, 0)
-        if need and not given:
-            scratch = _torch.empty(need, dtype=_torch.uint8, device=dev)
-            ws, n = scratch.data_ptr(), need
-        return _lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V,
-                               t_ptr, k_ptr, p_ptr, m_ptr, u_ptr, tokens.data_ptr(),
-                               None if probs is False else probs.data_ptr(), ws or None, n, s)
-
-    _check(_launch(index, stream, call), "vbq_sample")
+    if tokens is None:
+        tokens = _torch.empty(M, dtype=i32, device=dev)
+    if probs is None:
+        probs = _torch.empty(M, dtype=f32, device=dev)
+    token_ptr = _vector(tokens, "tokens", i32, M, index)
+    prob_ptr = None if probs is False else _vector(probs, "probs", f32, M, index)
+    ws, n = None, sample_workspace_size(M, V)
+    if workspace is not None:
+        ws, n = _scratch(workspace, index), workspace.numel()
+    elif n:
+        scratch = _torch.empty(n, dtype=_torch.uint8, device=dev)
+        ws = scratch.data_ptr()
+    _check(_lib.vbq_sample(M, V, _dtype_of(logits, "logits"), logits.data_ptr(), logits.stride(0) if M > 1 else V,
+                           t_ptr, k_ptr, p_ptr, m_ptr, u_ptr, token_ptr, prob_ptr, ws, n, _raw_stream(index)), "vbq_sample")
     return tokens, (None if probs is False else probs)
 
 
