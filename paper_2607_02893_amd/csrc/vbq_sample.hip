@@ -22,6 +22,8 @@
 //   gather  sums of what is before those bins, and a list of what is in them;
 //   token   one workgroup a row orders the list, finds the chunk that u falls into and the
 //           token in it.
+// In a graph 16 rows of 128256 fp32 logits with every kind of limit take 51 us (4.6 + 9.9 + 13 +
+// 24), one of 32000 28 (3.8 + 6.6 + 8.4 + 10.7); one workgroup a row took 551 and 201.
 // Launches rather than a row's last workgroup to arrive: that one needs the others' caches
 // written back, which took 30 us with 32 workgroups and 75 with 256, a launch takes 2.
 // Below x = -30.5 a weight is 0, so the bins end there.  A list that does not fit (a bin
