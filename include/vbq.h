@@ -626,9 +626,11 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
  *   workspace_dev    16-byte aligned scratch of at least
  *             vbq_kv_attention_workspace_size bytes, not shared by calls that
  *             may overlap (NULL where that is 0).
- * Sums and softmax statistics are fp32; a position's weight times its value
- * scale is rounded to fp16 (2^-11 of the term), fp32 queries are taken as two
- * fp16 terms, others as they are.  Sums are taken in a fixed order.
+ * Sums and softmax statistics are fp32.  Whatever the types of q and out, a
+ * position's weight times its value scale is rounded to fp16: by at most 2^-11 of
+ * the term, or, where that is more, 2^-31 of the row's largest weight times the
+ * largest value scale (of any group) that the row sees.  fp32 queries are taken
+ * as two fp16 terms, others as they are.  Sums are taken in a fixed order.
  * Errors: NULL, DESC, SHAPE (n_q_heads not a multiple of n_heads, more than
  * VBQ_KV_MAX_GROUP query heads a kv head, n_rows times that number above 2^30,
  * strides), UNSUPPORTED (types, scale), NONFINITE (scale), BUFFER, HIP. */

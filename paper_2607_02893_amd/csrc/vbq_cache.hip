@@ -428,20 +428,23 @@ __device__ __forceinline__ void load_block(Block<D>& k, const uint8_t* page, int
 // l % 16 of each tile: every quantity here, and o[d block] elements 4 (l / 16) + i.
 // Weights are held as 2^(score - mu - E): mu is within 8 of the row's largest score
 // so far (in powers of two; a sum is rescaled only where a score passes that), and
-// 2^E brings the values' largest scale so far into [2^6, 2^7), so that weight times
-// scale is an fp16 below 2^15 with 21 powers of two to its smallest normal.  The
-// product's rounding to fp16 (2^-11 of each term) is the only one below 32 bits.
+// 2^E brings the largest value scale that the row has seen so far into [2^6, 2^7), so
+// that weight times scale is an fp16 below 2^15 with 21 powers of two to its smallest
+// normal.  The product's rounding to fp16 (2^-11 of a term, or 2^-31 of the largest weight
+// times the largest scale where that is more) is the only one below 32 bits.  E is a
+// row's own: with one of a tile's, a later token's scale took the bits of earlier rows.
 template <int D, int NT, bool kTwoTerms>
 struct Rows {
   static constexpr int kGroups = D / 64;
   f16x8 q[NT][D / 32], q_low[kTwoTerms ? NT : 1][D / 32];
   float start[NT][kGroups];  // -8 2^-24 sum of q over a group
   f32x4 c;                   // (by tile) what a raw score is multiplied with to be a power of two
-  f32x4 mu, sum;             // (vectors: as arrays these three were kept in LDS, three accesses a block)
+  f32x4 mu, sum;
+  f32x4 e;                   // E + 21, the fp16 exponent field of the largest value scale
+  // (vectors: as arrays these four are kept in LDS, an access each a block)
   int visible[NT];
   f32x4 o[NT][D / 16];
   uint32_t one;              // 0x64006400
-  int e;                     // E + 21, the fp16 exponent field of the largest value scale
 
   // The row's elements times a power of two that puts the largest into [2^14, 2^15);
   // fp32 rows are split into two fp16 terms, the others are exact in one (unless
@@ -494,29 +497,37 @@ struct Rows {
       start[nt][grp] = -8.0f * 0x1p-24f * group_sum(total);
     }
     mu[nt] = -__builtin_inff();
-    sum[nt] = 0.0f;
+    sum[nt] = e[nt] = 0.0f;
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[nt][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
   __device__ __forceinline__ float bias(int nt) const {
-    return (mu[nt] == -__builtin_inff() ? 0.0f : mu[nt]) + (float)(e - 21);
+    return (mu[nt] == -__builtin_inff() ? 0.0f : mu[nt]) + (e[nt] - 21.0f);
+  }
+
+  // The exponent field of the largest of a lane's value scales (by slot), without those that `seen` clears.
+  __device__ __forceinline__ float largest(const Block<D>& k, const u32x4& seen) const {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4 * kGroups; ++i) top = larger16(top, k.vs[i / 4][i % 4] & seen[i % 4]);
+    top = ((top & 0xffffu) > (top >> 16) ? top & 0xffffu : top >> 16) >> 10;
+    if (top >= 31) {  // a NaN among them: the others set the range
+      top = 0;
+#pragma unroll
+      for (int i = 0; i < 4 * kGroups; ++i) {
+        const uint32_t w = k.vs[i / 4][i % 4] & seen[i % 4], lo = (w >> 10) & 31u, hi = (w >> 26) & 31u;
+        top = lo < 31 && lo > top ? lo : top;
+        top = hi < 31 && hi > top ? hi : top;
+      }
+    }
+    return (float)top;
   }
 
   // One block of 32 positions from `pos` on; edge: some of them are hidden from some row.
-  // Hidden positions get the score -inf and their product with the value scale is 0,
-  // whatever their memory holds.
-  __device__ __forceinline__ void block(Block<D>& k, int pos, int end, int g, bool edge) {
-    if (edge) {
-#pragma unroll
-      for (int grp = 0; grp < kGroups; ++grp) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          // nothing has been written at positions from `end` on
-          if (pos + 16 * (i >> 2) + 4 * g + (i & 3) >= end) k.vs[grp][i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
-        }
-      }
-    }
+  // Hidden positions get the score -inf, their product with the value scale is 0 and
+  // the scale does not count for E, whatever their memory holds.
+  __device__ __forceinline__ void block(Block<D>& k, int pos, int g, bool edge) {
     float x[NT][8];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -553,45 +564,54 @@ struct Rows {
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (pos + 16 * (i >> 2) + 4 * g + (i & 3) >= visible[nt]) x[nt][i] = -__builtin_inff();
+          if (pos + 16 * (i >> 2) + 4 * g + (i & 3) >= visible[nt]) {
+            x[nt][i] = -__builtin_inff();
+            if constexpr (NT == 1) {
+#pragma unroll
+              for (int grp = 0; grp < kGroups; ++grp) k.vs[grp][i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+            }
+          }
         }
       }
     }
 
     // ---- the bias moves where a score passes it by 2^8, or a value scale the largest so far
-    uint32_t top = 0;
+    float top[NT];
+    if (NT > 1 && edge) {  // (two rows of a lane: what the one sees the other may not)
 #pragma unroll
-    for (int i = 0; i < 4 * kGroups; ++i) top = larger16(top, k.vs[i / 4][i % 4]);
-    top = ((top & 0xffffu) > (top >> 16) ? top & 0xffffu : top >> 16) >> 10;
-    if (top >= 31) {  // a NaN among them: rows that do not see it keep the others' range
-      top = 0;
+      for (int nt = 0; nt < NT; ++nt) {
+        u32x4 seen = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
 #pragma unroll
-      for (int i = 0; i < 4 * kGroups; ++i) {
-        const uint32_t w = k.vs[i / 4][i % 4], lo = (w >> 10) & 31u, hi = (w >> 26) & 31u;
-        top = lo < 31 && lo > top ? lo : top;
-        top = hi < 31 && hi > top ? hi : top;
+        for (int i = 0; i < 8; ++i) {
+          if (pos + 16 * (i >> 2) + 4 * g + (i & 3) >= visible[nt]) seen[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+        }
+        top[nt] = largest(k, seen);
       }
+    } else {
+      top[0] = largest(k, u32x4{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu});
+#pragma unroll
+      for (int nt = 1; nt < NT; ++nt) top[nt] = top[0];
     }
-    bool grow = (int)top > e;
+    bool grow = false;
     float most[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float low = max3(max3(x[nt][0], x[nt][1], x[nt][2]), x[nt][3], x[nt][4]);
       most[nt] = max3(low, max3(x[nt][5], x[nt][6], x[nt][7]), x[nt][7]) * c[nt];
-      grow |= most[nt] > mu[nt] + 8.0f;
+      grow |= most[nt] > mu[nt] + 8.0f || top[nt] > e[nt];
     }
     if (__builtin_amdgcn_ballot_w64(grow)) {
-      const int en = (int)group_max((float)((int)top > e ? (int)top : e));
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
+        const float en = group_max(top[nt] > e[nt] ? top[nt] : e[nt]);
         const float m = group_max(most[nt]), now = m > mu[nt] + 8.0f ? m : mu[nt];
-        const float alpha = mu[nt] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((mu[nt] - now) + (float)(e - en));
+        const float alpha = mu[nt] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((mu[nt] - now) + (e[nt] - en));
         mu[nt] = now;
+        e[nt] = en;
         sum[nt] *= alpha;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[nt][d] *= alpha;
       }
-      e = en;
     }
 
     // ---- weights, and their products with the value scales as the second product's operand
@@ -608,7 +628,7 @@ struct Rows {
           w[nt][grp][i] = (_Float16)__builtin_fmaf(p, (float)__builtin_bit_cast(f16x8, k.vs[grp])[i], 0.0f);
       }
     }
-    if (edge) {
+    if (NT > 1 && edge) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -663,7 +683,6 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
   for (uint32_t tile = gridDim.z - 1 - blockIdx.z; tile * kRows < n_rows; tile += gridDim.z) {
     const uint32_t base = tile * kRows;
     Rows<D, NT, kTwoTerms> r;
-    r.e = 0;
     asm("v_mov_b32 %0, 0x64006400" : "=v"(r.one));
     const uint32_t last = base + 16 * NT < n_rows ? base + 16 * NT : n_rows;
     auto seen = [&](uint32_t row) {
@@ -710,7 +729,7 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
       } else {
         half = 1;
       }
-      r.block(k, pos, (int)s.end, g, pos + 32 > least);
+      r.block(k, pos, g, pos + 32 > least);
       if (page < stop) load(k, id, half);
     }
 
