@@ -150,10 +150,11 @@ __device__ __forceinline__ float quantize8(const float (&f)[8], int (&code)[8]) 
   // below zero would be a score of -inf, a position quietly left out
   float s = amax == amax ? fp16_from_double((double)amax / 7.0) : amax;
   s = s < __builtin_inff() ? s : __builtin_nanf("");
-  const float r = s > 0.0f ? __builtin_amdgcn_rcpf(s) : 0.0f;
+  // with s = 0 every level is 0: r is, and a NaN keeps exact_rne, which a neighbour may call for, from stepping
+  const float r = s > 0.0f ? __builtin_amdgcn_rcpf(s) : 0.0f, by = s > 0.0f ? s : __builtin_nanf("");
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    code[i] = (int)(level4(f[i], s, r) + 8.0f);  // (some code where the scale is NaN)
+    code[i] = (int)(level4(f[i], by, r) + 8.0f);  // (some code where the scale is NaN)
   }
   return s;
 }
