@@ -618,7 +618,9 @@ vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
  * them, over the positions p from 0 up to the row's own (so its own key and
  * value are to be appended first).  A row that sees no position (before
  * position 0, or all its pages outside the cache) gives zeros; what the cache
- * holds at positions that a row does not see does not matter, NaN included.
+ * holds at positions that a row does not see does not matter, NaN included.  A
+ * NaN scale at a position that it sees, however little that weighs, makes the
+ * row NaN (a key's) or its 64 elements of that group (a value's).
  *   q_dev, out_dev   [n_rows][n_q_heads][D] of q_type, out_type, with row and
  *             head strides in elements (multiples of 8; out's >= D), 16-byte
  *             aligned; they may not overlap.  |q| below 2^60.

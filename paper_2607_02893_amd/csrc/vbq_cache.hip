@@ -758,9 +758,9 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
       }
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        // (a wave that saw nothing of the row, or only NaN biases, adds its sum as it is)
-        f[w] = f[w] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(f[w] - top);
-        sum += sum_lds[w][i] * f[w];
+        // -1: a wave that saw nothing of the row.  One that weighs nothing still adds its sums: 0 times NaN is NaN.
+        f[w] = f[w] == -__builtin_inff() ? -1.0f : __builtin_amdgcn_exp2f(f[w] - top);
+        sum += f[w] < 0.0f ? 0.0f : sum_lds[w][i] * f[w];
       }
       const int64_t row = s.row0 + ri / group;
       const int64_t hq = hq0 + ri % group;
@@ -772,7 +772,7 @@ __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_att
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          if (f[w] != 0.0f) v += *(const f32x4*)&o_lds[w][i][4 * (sub + kLanes * (d / 4))] * f[w];
+          if (f[w] >= 0.0f) v += *(const f32x4*)&o_lds[w][i][4 * (sub + kLanes * (d / 4))] * f[w];
         }
         const int el = 4 * (sub + kLanes * (d / 4));
         if (a.splits > 1) *(f32x4*)(a.part + (rh * a.splits + split) * D + el) = v;
@@ -806,25 +806,26 @@ __global__ __launch_bounds__(kWaves * 64) void vbq_kv_join_kernel(AttnArgs a) {
       float top = bias;
 #pragma unroll
       for (int d = 32; d >= 1; d >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, d, 64));
-      const float f = n == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(bias - top);
+      const float f = n == 0.0f ? -1.0f : __builtin_amdgcn_exp2f(bias - top);  // -1: it saw nothing of the row
       f_lds[tid] = f;
-      sum = n * f;
+      sum = n == 0.0f ? 0.0f : n * f;
 #pragma unroll
       for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
     }
     __syncthreads();
-    // a part that saw nothing was not written: the first is read in its place, times 0
+    // a part that saw nothing was not written: the first is read in its place and not added (one that
+    // weighs nothing is: 0 times NaN is NaN)
     f32x4 part[kTurns];
 #pragma unroll
     for (int j = 0; j < kTurns; ++j) {
       const int p = side + j * kSide;
-      part[j] = *(const f32x4*)(a.part + (rh * a.splits + (f_lds[p] != 0.0f ? p : 0)) * D + el);
+      part[j] = *(const f32x4*)(a.part + (rh * a.splits + (f_lds[p] >= 0.0f ? p : 0)) * D + el);
     }
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < kTurns; ++j) {
       const float f = f_lds[side + j * kSide];
-      if (f != 0.0f) v += part[j] * f;
+      if (f >= 0.0f) v += part[j] * f;
     }
     *(f32x4*)&o_lds[side][el] = v;
     __syncthreads();
