@@ -25,6 +25,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // 512 / 256 threads: one row 3.6 / 4.3, 16 rows 3.8 / 5.8, 256 rows 4.3 / 5.0, 4096 rows 27.7 / 27.3).
 constexpr int64_t kFewRows = 256;
 
+// Rows of a launch, a workgroup each: a grid holds fewer than 2^32 threads along a dimension.
+constexpr int64_t kRowsAtOnce = (int64_t)1 << 22;
+
 struct NormArgs {
   const void* residual;
   const void* y;       // may be null
@@ -200,14 +203,23 @@ vbq_status vbq_add_norm(int64_t n_rows, int64_t K, int32_t res_type, const void*
     if ((uintptr_t)r.p % size_of(r.type)) return VBQ_ERR_BUFFER;
     vec = vec && (uintptr_t)r.p % 16 == 0 && r.ld % 8 == 0;
   }
-  NormArgs a{residual_dev, y_dev, weight_dev, h_dev, x_dev, ldr, ldy, ldh, ldx, (int32_t)K, res_type, y_type,
-             weight_type, x_type, vec ? 1 : 0, eps};
-  void* args[] = {&a};
   const int threads = n_rows <= kFewRows ? 512 : 256;
   const bool shorter = K <= 16 * threads;
   const void* f = threads == 512 ? (shorter ? (const void*)vbq_add_norm_kernel<512, 2> : (const void*)vbq_add_norm_kernel<512, 4>)
                                  : (shorter ? (const void*)vbq_add_norm_kernel<256, 2> : (const void*)vbq_add_norm_kernel<256, 4>);
-  return vbq_detail_hip_status(hipLaunchKernel(f, dim3((unsigned)n_rows), dim3((unsigned)threads), args, 0, (hipStream_t)stream));
+  for (int64_t row = 0; row < n_rows; row += kRowsAtOnce) {
+    const int64_t n = n_rows - row < kRowsAtOnce ? n_rows - row : kRowsAtOnce;
+    auto from = [&](const void* p, int64_t ld, int32_t type) {
+      return p ? (uint8_t*)p + (size_t)row * (size_t)ld * size_of(type) : nullptr;
+    };
+    NormArgs a{from(residual_dev, ldr, res_type), from(y_dev, ldy, y_type), weight_dev, from(h_dev, ldh, res_type),
+               from(x_dev, ldx, x_type), ldr, ldy, ldh, ldx, (int32_t)K, res_type, y_type, weight_type, x_type, vec ? 1 : 0, eps};
+    void* args[] = {&a};
+    const vbq_status st =
+        vbq_detail_hip_status(hipLaunchKernel(f, dim3((unsigned)n), dim3((unsigned)threads), args, 0, (hipStream_t)stream));
+    if (st != VBQ_OK) return st;
+  }
+  return VBQ_OK;
 }
 
 }  // extern "C"
