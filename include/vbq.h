@@ -547,6 +547,7 @@ vbq_status vbq_add_norm(int64_t n_rows, int64_t K, int32_t res_type,
 #define VBQ_KV_MAX_SEQS 65535
 #define VBQ_KV_MAX_ROWS (((int64_t)1) << 30)
 #define VBQ_KV_MAX_TABLE (1 << 24)    /* pages of one sequence                 */
+#define VBQ_KV_MAX_PARTS (1 << 18)    /* sums of D floats in a workspace       */
 
 /* Host-side description of a cache (plain old data). */
 typedef struct vbq_kv_desc {
@@ -579,9 +580,10 @@ typedef struct vbq_kv_batch {
   const int32_t* seq_len;         /* device int32[n_seqs]                      */
   int64_t n_rows;                 /* 0 .. VBQ_KV_MAX_ROWS                      */
   int32_t max_rows;               /* rows of the sequence with the most.  With */
-  int32_t max_len;                /* row_start it only sizes the launch, as    */
-} vbq_kv_batch;                   /* max_len (positions) does: a wrong value
-                                     costs time, not correctness               */
+  int32_t max_len;                /* row_start it only sizes the launch and    */
+} vbq_kv_batch;                   /* the workspace, as max_len (positions)
+                                     does: a wrong value costs time, and
+                                     workspace, not correctness                */
 
 /* Quantizes the rows of k and v into their positions' places in the cache.
  * k, v: [n_rows][n_heads][D] of one type with row strides ldk, ldv and head
@@ -606,7 +608,8 @@ vbq_status vbq_kv_dequant(const vbq_kv_desc* desc, const void* cache_dev,
                           void* stream);
 
 /* Bytes of vbq_kv_attention's device workspace for this batch (0 where it
- * needs none): a function of desc, n_q_heads and the batch's host fields.
+ * needs none): a function of desc, n_q_heads and the batch's host fields, and
+ * no more than VBQ_KV_MAX_PARTS * (D + 2) floats whatever these are.
  * Errors: NULL, DESC, SHAPE. */
 vbq_status vbq_kv_attention_workspace_size(const vbq_kv_desc* desc,
                                            const vbq_kv_batch* batch,

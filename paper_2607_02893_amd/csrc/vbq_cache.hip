@@ -907,6 +907,16 @@ Plan plan_of(const vbq_kv_desc* d, const vbq_kv_batch* b, int group) {
   part = part < most_parts ? most_parts : part;
   p.split_pages = (int)part;
   p.splits = pages > part ? (int)((pages + part - 1) / part) : 1;
+  // A max_rows that is right (and no rows but the sequences') keeps n_rows * query heads * splits below
+  // 16 * 1536.  Where it is far too small, the parts' sums would fill the memory (8192 rows of 32 heads
+  // said to be one a sequence: 8.7 GB): fewer parts then, and tiles for what the rows are on average.
+  const int64_t row_heads = b->n_rows * d->n_heads * (int64_t)group;
+  if (p.splits > 1 && row_heads * p.splits > VBQ_KV_MAX_PARTS) {
+    const int64_t fewer = VBQ_KV_MAX_PARTS / row_heads, mean = (b->n_rows * group / b->n_seqs + per) / per;
+    p.splits = fewer > 1 ? (int)fewer : 1;
+    if (p.tiles < mean) p.tiles = (int)(mean < 16384 ? mean : 16384);
+    if (p.tiles > most) p.tiles = most > 1 ? (int)most : 1;
+  }
   return p;
 }
 
