@@ -42,6 +42,7 @@ vbq_status vbq_detail_hip_status(hipError_t e);
 namespace {
 
 using vbq::Batch;
+using vbq::blocks_of;
 using vbq::code_bit;
 using vbq::exact_rne;
 using vbq::fp16_from_double;
@@ -968,9 +969,8 @@ vbq_status vbq_kv_append(const vbq_kv_desc* desc, void* cache_dev, const vbq_kv_
   if (!aligned(cache_dev, 256) || !aligned(k_dev, 16) || !aligned(v_dev, 16)) return VBQ_ERR_BUFFER;
   AppendArgs a{batch_of(batch), (uint8_t*)cache_dev, desc->n_pages, desc->n_heads, type, k_dev, v_dev, ldk, hsk, ldv, hsv};
   void* args[] = {&a};
-  const int64_t rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
-  const int64_t blocks = (rows + 31) / 32 + (rows > 1 ? 1 : 0);  // (a row's block may begin before it)
-  const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), (unsigned)desc->n_heads, (unsigned)batch->n_seqs);
+  const dim3 grid((unsigned)blocks_of(batch->max_rows, batch->n_rows, desc->n_heads, batch->n_seqs), (unsigned)desc->n_heads,
+                  (unsigned)batch->n_seqs);
   const void* f = desc->head_dim == 64    ? (const void*)vbq_kv_append_kernel<64>
                   : desc->head_dim == 128 ? (const void*)vbq_kv_append_kernel<128>
                                           : (const void*)vbq_kv_append_kernel<256>;
@@ -987,9 +987,8 @@ vbq_status vbq_kv_dequant(const vbq_kv_desc* desc, const void* cache_dev, const 
   if (!aligned(cache_dev, 256) || !aligned(k_dev, 16) || !aligned(v_dev, 16)) return VBQ_ERR_BUFFER;
   DequantArgs a{batch_of(batch), (const uint8_t*)cache_dev, desc->n_pages, desc->n_heads, k_dev, v_dev};
   void* args[] = {&a};
-  const int64_t rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
-  const int64_t blocks = (rows + 31) / 32 + (rows > 1 ? 1 : 0);  // (a row's block may begin before it)
-  const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), (unsigned)desc->n_heads, (unsigned)batch->n_seqs);
+  const dim3 grid((unsigned)blocks_of(batch->max_rows, batch->n_rows, desc->n_heads, batch->n_seqs), (unsigned)desc->n_heads,
+                  (unsigned)batch->n_seqs);
   const void* f = desc->head_dim == 64    ? (const void*)vbq_kv_dequant_kernel<64>
                   : desc->head_dim == 128 ? (const void*)vbq_kv_dequant_kernel<128>
                                           : (const void*)vbq_kv_dequant_kernel<256>;

@@ -92,4 +92,16 @@ VBQ_HD int64_t page_id(const Batch& a, int64_t n_pages, int b, int64_t page) {
   return id >= 0 && (int64_t)id < n_pages ? id : -1;
 }
 
+// Workgroups that share the 32-position blocks of each head and sequence in the append and the
+// read-back, each taking every so-manieth: as many as the rows need, but no more than 2^16, nor
+// than makes 2^22 over all heads and sequences (with max_rows from the longest of many sequences,
+// or a guess, nearly all would have nothing to do: 2^42 within the limits of a batch).
+VBQ_HD int64_t blocks_of(int64_t max_rows, int64_t n_rows, int64_t heads, int64_t n_seqs) {
+  const int64_t rows = max_rows < n_rows ? max_rows : n_rows;
+  const int64_t blocks = (rows + 31) / 32 + (rows > 1 ? 1 : 0);  // (a row's block may begin before it)
+  const int64_t share = ((int64_t)1 << 22) / (heads * n_seqs), most = share > 1 ? share : 1;
+  const int64_t few = blocks < 65536 ? blocks : 65536;
+  return few < most ? few : most;
+}
+
 }  // namespace vbq

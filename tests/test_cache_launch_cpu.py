@@ -1,11 +1,14 @@
-"""Without a GPU: what a call on the cache asks for in memory, whatever its hints say."""
+"""Without a GPU: what a call on the cache asks for in memory and workgroups, whatever its hints say."""
 
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 
 from paper_2607_02893_amd import vbq
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 A = 1 << 20  # an address that nothing here looks at
 MOST = 1 << 18  # VBQ_KV_MAX_PARTS
 
@@ -46,3 +49,33 @@ def test_right_hints_stay_below_the_bound():
         assert n <= 16 * 1536 * (D + 2) * 4
         split += n > 0
     assert split > 1000
+
+
+HOST = r"""
+#include "paper_2607_02893_amd/csrc/vbq_cache.hpp"
+#include <cstdio>
+#include <cstdlib>
+#include <initializer_list>
+#define NEED(c) do { if (!(c)) { std::printf("line %d: %s\n", __LINE__, #c); std::exit(1); } } while (0)
+int main() {
+  const int64_t counts[] = {1, 2, 31, 32, 33, 1000, 65535, 1 << 20, 1 << 30};
+  for (int64_t max_rows : counts) for (int64_t n_rows : counts) for (int64_t heads : {1, 3, 8, 1024}) for (int64_t seqs : {1, 16, 1000, 65535}) {
+    const int64_t n = vbq::blocks_of(max_rows, n_rows, heads, seqs), all = n * heads * seqs;
+    const int64_t rows = max_rows < n_rows ? max_rows : n_rows;
+    NEED(n >= 1 && n <= 65536 && n * 256 < (1ll << 32));
+    NEED(all <= (1 << 22) || n == 1);
+    // as many as the rows' blocks where those are few
+    const int64_t need = rows == 1 ? 1 : (rows + 31) / 32 + 1;
+    if (need <= 65536 && need * heads * seqs <= (1 << 22)) NEED(n == need);
+  }
+  std::printf("ok\n");
+}
+"""
+
+
+def test_workgroups_are_bounded_whatever_the_hints(tmp_path):
+    src, exe = tmp_path / "grid.cpp", tmp_path / "grid"
+    src.write_text(HOST)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", ROOT, str(src), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0 and out.stdout.strip() == "ok", out.stdout

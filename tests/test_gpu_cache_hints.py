@@ -1,11 +1,13 @@
-"""Hints so far off that the parts' sums would outgrow the workspace: the same result in fewer parts."""
+"""Hints so far off that the parts' sums would outgrow the workspace, or the grid all bounds: the same
+result in fewer parts, the same bytes from fewer workgroups."""
 
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
-from tests.test_gpu_cache import Case, _check_attention, _rows, _say  # noqa: E402
+from oracle import decode as odec  # noqa: E402
+from tests.test_gpu_cache import Case, _check_attention, _dev, _np, _rows, _say  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +35,24 @@ def test_many_rows_said_to_be_one(vbq, d, group, lens, rows, max_len):
     assert 0 < need <= (1 << 18) * (d + 2) * 4
     out = c.cache.attention(q, b, out_dtype=torch.float32)
     _check_attention(out, q, c, rows, d ** -0.5, "f32", what="hints")
+
+
+def test_many_sequences_and_a_far_hint(vbq):
+    """Each workgroup goes on to the blocks that a smaller grid leaves: two long sequences of 4000, one row elsewhere."""
+    rng = np.random.default_rng(40)
+    n, hkv, d = 4000, 64, 64
+    rows = np.zeros(n, dtype=np.int64)
+    rows[[7, 3999]] = [900, 700]
+    rows[100] = 1
+    starts = np.concatenate([[0], np.cumsum(rows)])
+    total = int(starts[-1])
+    table = np.full((n, 15), -1, dtype=np.int32)
+    table[7], table[3999, :11], table[100, 0] = np.arange(15), np.arange(15, 26), 26
+    lens = rows.astype(np.int32)
+    few = vbq.KVCache(27, hkv, d)
+    k, v = _rows(rng, total, hkv, d, "f16"), _rows(rng, total, hkv, d, "f16")
+    far = vbq.KVBatch(_dev(table), _dev(lens), _dev(starts), n_rows=total, max_rows=2 ** 31 - 1)
+    _say("append, 4000 sequences, far hint")
+    few.append(k, v, far)
+    dk, dv = few.dequant(far)
+    assert np.array_equal(_np(dk), odec.kv_values(_np(k))) and np.array_equal(_np(dv), odec.kv_values(_np(v)))
