@@ -506,7 +506,8 @@ typedef enum vbq_dtype { VBQ_F32 = 0, VBQ_F16 = 1, VBQ_BF16 = 2 } vbq_dtype;
  *               their pointers NULL).
  * Pointers are aligned to their element; rows that begin at 16 bytes (pointer
  * 16-byte aligned, strides and K multiples of 8) are read and written in
- * 16-byte runs.  A row's sum is taken in a fixed order.  n_rows == 0 does
+ * 16-byte runs.  A row's sum of h^2 is taken in fp32 and in a fixed order: where
+ * it passes fp32's range (|h| near 2^64), finite h give 0.  n_rows == 0 does
  * nothing.  Errors: SHAPE (K outside [1, VBQ_NORM_MAX_K], n_rows outside
  * [0, 2^31), a stride < K), UNSUPPORTED (unknown type, eps < 0), NONFINITE
  * (eps), NULL (residual or x), BUFFER (misaligned), HIP. */
@@ -567,7 +568,8 @@ vbq_status vbq_kv_layout(int64_t n_pages, int32_t n_heads, int32_t head_dim,
  * out); sequence b owns rows row_start[b] .. row_start[b+1]-1, or max_rows rows
  * each with row_start NULL (n_rows == n_seqs * max_rows then).  seq_len[b]
  * counts its positions, this call's rows included: the last of its n rows is at
- * position seq_len[b] - 1, its row r at seq_len[b] - n + r.  The arrays are
+ * position seq_len[b] - 1, its row r at seq_len[b] - n + r, n being the rows of
+ * row_start[b] .. row_start[b+1]-1 that lie in [0, n_rows).  The arrays are
  * device memory, read when the kernel runs.  Whatever they hold, rows outside
  * [0, n_rows), positions below 0 or beyond table_stride pages, and pages
  * outside [0, n_pages) are neither read nor written; what that leaves out is

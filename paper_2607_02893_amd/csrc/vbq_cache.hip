@@ -25,9 +25,11 @@
 // their lane, and every code load is 16 bytes a lane, 1 KiB a wave.
 //
 // One token over long sequences is bound by the pages' reads and, nearly as much, by vector issue
-// (131073 positions of 8 heads of 128: 32 us and 4.8 for the join, 3.8 TB/s; the reads alone 25, the issue
-// alone 15), prompts by vector issue alone (2 x 2048 rows behind 4096 positions, 32 heads: 524 us, 480
-// TFLOP/s; 348 instructions a block of 32 positions and 32 rows, 112 of them converting codes).
+// (131073 positions of 8 heads of 128: 33 us and 4.7 for the join, 3.8 TB/s; the reads alone 25, the issue
+// alone 15), prompts most by vector issue (2048 and 1371 rows over 6144 and 4099 positions, 32 heads: 527 us,
+// 470 TFLOP/s; 353 instructions a block of 32 positions and 32 rows, 112 of them converting codes; vector
+// units are active for 302 of the 527 us, matrix cores for 99, and of the waves' cycles 22 % wait for memory
+// and 24 % for issue).
 
 #include <hip/hip_runtime.h>
 
@@ -651,9 +653,7 @@ struct Rows {
   }
 };
 
-__device__ __forceinline__ int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// A row's result, or its part where the positions are split: the sums, their bias and the sum of weights.
+// What the join needs of a row's part beside its D sums: their bias and the sum of weights (0: it saw nothing).
 template <int D>
 __device__ __forceinline__ void store_bias(const AttnArgs& a, int64_t row_head, int split, float bias, float sum) {
   float* at = a.part + a.batch.n_rows * a.heads * a.group * (int64_t)a.splits * D + 2 * (row_head * a.splits + split);
@@ -665,9 +665,12 @@ constexpr int waves_per_simd(int D, int NT) { return NT > 1 || D > 128 ? 2 : D >
 
 // A workgroup takes a tile of 16 NT rows (query heads of one kv head, row by row) and a part of
 // the positions; its waves take every fourth page each and join at the end, a lane's sums through LDS.
-// Rows of their own for the waves (no join, each page read by all four) came to the same on grids
-// that fill the chip (2 x 2048 rows of 32 heads over 6144 positions 514 us, so 527) and to two to six times
-// as long on smaller ones (256 rows over 16384: 284 us, so 46), where a wave walks all positions.
+// Rows of their own for the waves (no join, each page read by all four) came to much the same on grids
+// that fill the chip (the two prompts above 505 us, so 524 at the time) and to four to five times as long
+// on smaller ones (64 rows of 32 heads over 16384 positions: 284 us, so 54), where a wave walks all positions.
+// fp32 queries keep twice the registers: with 64 and 128 elements 2 to 8 values wait in scratch memory
+// outside the loop over pages, with 256 elements 24, four of them read back within it (sixteen sequences:
+// 36.7 us, 30.2 with 16-bit queries; the prompts 589 and 527).
 template <int D, int NT, bool kTwoTerms>
 __global__ __launch_bounds__(kWaves * 64, waves_per_simd(D, NT)) void vbq_kv_attention_kernel(AttnArgs a) {
   using P = PageOf<D>;

@@ -26,8 +26,11 @@
 // 24), one of 32000 28 (3.8 + 6.6 + 8.4 + 10.7); one workgroup a row took 551 and 201.
 // Launches rather than a row's last workgroup to arrive: that one needs the others' caches
 // written back, which took 30 us with 32 workgroups and 75 with 256, a launch takes 2.
-// Below x = -30.5 a weight is 0, so the bins end there.  A list that does not fit (a bin
-// holds thousands of equal logits) sends its row through the row kernel's steps instead.
+// Rows of 4096 logits take 9.6 us without a limit, 18 with top-k, 24 with top-p and 32 with both.
+// Below x = -30.5 a weight is 0, so the bins end there.  A list that does not fit (more than kCap
+// logits within 1/16 of T, equal or not: 262144 of standard deviation T, cut by top-p near
+// their peak) sends its row through the row kernel's steps, over global memory, instead: 1.1 ms, where
+// the same row with a standard deviation of 3 T takes 49 us.
 
 #include <hip/hip_runtime.h>
 
@@ -43,7 +46,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 1024;
 constexpr int kWavesRow = kThreads / 64;  // 16: a value a wave is a row of lanes
-constexpr double kOne = 0x1p43;  // the weight of the largest logit; 2^20 of them stay below 2^63
+constexpr double kOne = 0x1p43;  // the weight of the largest logit; 2^20 of them are at most 2^63
 constexpr double kLeast = -30.5; // below ln 2^-44 = -30.498 a weight rounds to 0
 constexpr double kNone = -1e300;
 constexpr int kBinsPerUnit = 16, kBins = 489;  // (the last holds x = kLeast alone)

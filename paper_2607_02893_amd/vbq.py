@@ -831,8 +831,9 @@ class KVBatch:
     [n_seqs + 1], the first row of each sequence and the end of the last; None:
     max_rows rows each.  n_rows: rows of the call's tensors (n_seqs * max_rows
     by default).  max_rows, max_len: the most rows and positions of a sequence
-    (with `rows`, and for max_len always, they size the launch only; max_len
-    defaults to what the table holds).  The tensors may change between calls
+    (with `rows`, and for max_len always, they size the launch and the workspace only,
+    so a wrong one costs time: give max_rows with prompts, and a max_len where the table
+    holds several times what the sequences have; it defaults to what the table holds).  The tensors may change between calls
     (a captured graph reads them anew); they must stay alive until the call has run."""
 
     def __init__(self, page_table, seq_len, rows=None, n_rows=None, max_rows=1, max_len=None):
